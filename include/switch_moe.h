@@ -299,6 +299,112 @@ int switch_moe_launches_per_step(const switch_moe_config* cfg, int32_t* launches
  * gap between the forward and the backward pass, is 0). */
 int switch_moe_stage_launches(const switch_moe_config* cfg, int32_t* launches_out);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Operators around the layer: what the rest of a Switch model's feed-forward path and its training loop need.  The
+ * conventions above hold (device pointers, one stream, status codes, gradients overwritten), with two differences:
+ * tensors are rows at a stated distance (ld.. fields, 0 = dense; a distance in bytes is a multiple of 16, and what lies
+ * between a row's end and the next row is neither read nor written), and the arithmetic is float32 or wider with one
+ * rounding of each result to the tensor's type.
+ *
+ * Dropout.  The mask is a function of the element's place and a state, and is never stored: forward and backward
+ * compute it where they need it.  `rng` is DEVICE uint64[2], read when the kernel runs, so that a captured graph draws
+ * a new mask at every replay after the caller has advanced rng[1] on the stream.  Row r's elements 8 j .. 8 j + 7 share
+ * one call of Philox4x32-10 (Salmon et al., 2011) with key = rng[0] (low word first) and counter = {low word of b,
+ * high word of b + site . 2^16, low word of rng[1], high word of rng[1]}, b = r . ceil(columns / 8) + j.  Element
+ * 8 j + i has the 16 bits [16 i, 16 i + 16) of the 128-bit result; it is dropped if they are below
+ * q = floor(rate . 65536 + 1/2), and multiplied by 65536 / (65536 - q) otherwise.  `site` (0 .. 65535) tells the places
+ * of a model apart that share a state.  The rates lie in [0, 1); a rate whose q is 65536 is refused, one whose q is 0
+ * drops nothing. */
+
+enum switch_moe_activation { SWITCH_MOE_ACT_NONE = 0, SWITCH_MOE_ACT_RELU = 1, SWITCH_MOE_ACT_GELU = 2 /* z Phi(z) */ };
+
+/* Dense product with its epilogue, the FFN and projections of the layers between Switch layers:
+ *   z = x W + bias,   y = residual + dropout(activation(z)). */
+typedef struct switch_moe_linear_config {
+  int32_t M;                 /* rows (tokens) of x and y; 0 is an empty call */
+  int32_t K;                 /* columns of x, rows of W */
+  int32_t N;                 /* columns of W and y */
+  int32_t dtype;             /* switch_moe_dtype of x, W, y, residual, pre, dy, dx, dW; bias and dbias are float32 */
+  int32_t activation;        /* switch_moe_activation */
+  int32_t site;              /* dropout: place in the model */
+  float dropout;             /* rate; 0: none, and rng may be NULL */
+  int32_t ldx, ldw, ldy;     /* elements between rows of x and dx; of W and dW; of y, residual, pre and dy; 0: K, N, N */
+  int32_t reserved[2];       /* must be 0 */
+} switch_moe_linear_config;
+
+/* HOST call.  Bytes of device workspace (1024-byte aligned) of a forward call, or with backward != 0 of a forward or a
+ * backward call.  Nothing in it survives a call; calls that share it must be ordered on one stream. */
+int switch_moe_linear_workspace_bytes(const switch_moe_linear_config* cfg, int32_t backward, size_t* bytes_out);
+
+/* Forward.  x [M,K]; W [K,N]; bias float32[N] or NULL; residual [M,N] or NULL (may be y itself); rng: see above;
+ * y [M,N] (out); pre [M,N] (out) receives z for the backward pass, or NULL.  x, W and bias may not overlap y or pre.
+ * bf16: products on the tensor cores, float32 sums; f32: the same cores on sums of exact bfloat16 parts, error against
+ * float64 no larger than float32 FMA's (a result that is not finite, or from 2^80 on, is formed by FMA). */
+int switch_moe_linear_fwd(const switch_moe_linear_config* cfg, const void* x, const void* W, const float* bias,
+                          const void* residual, const uint64_t* rng, void* y, void* pre, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/* Backward, for the upstream gradient dy [M,N] of y and the same x, W, rng contents and site:
+ *   dz = dropout(dy) . activation'(pre),  dx = dz W^T,  dW = x^T dz,  dbias = sum of dz over rows;
+ * the residual's gradient is dy itself.  pre: what the forward call wrote (for RELU any tensor with the same signs, such
+ * as y without dropout and residual); NULL only for ACT_NONE.  Each of dx, dW, dbias may be NULL: not wanted.  x may be
+ * NULL without dW, W without dx.  bf16: dx and dW are products of dz rounded to bfloat16, dbias sums it unrounded.
+ * M = 0 writes zeros to dW and dbias. */
+int switch_moe_linear_bwd(const switch_moe_linear_config* cfg, const void* dy, const void* x, const void* W,
+                          const void* pre, const uint64_t* rng, void* workspace, size_t workspace_bytes, void* dx,
+                          void* dW, float* dbias, void* stream);
+
+/* Synchronises `stream` and reads the status word that the last call left in the workspace; as
+ * switch_moe_check_device_status. */
+int switch_moe_linear_check_device_status(const switch_moe_linear_config* cfg, void* workspace, int32_t* info_out,
+                                          void* stream);
+
+/* Dropout of a [rows, cols] tensor, on its own. */
+typedef struct switch_moe_dropout_config {
+  int32_t rows, cols;        /* rows = 0 is an empty call */
+  int32_t ld;                /* elements between rows of every tensor of the call; 0: cols */
+  int32_t dtype;             /* switch_moe_dtype */
+  int32_t site;
+  float rate;
+  int32_t reserved[2];       /* must be 0 */
+} switch_moe_dropout_config;
+
+/* y = residual + dropout(x).  residual may be NULL; y may be x or residual. */
+int switch_moe_dropout_fwd(const switch_moe_dropout_config* cfg, const void* x, const void* residual,
+                           const uint64_t* rng, void* y, void* stream);
+/* dx = dropout(dy) with the same mask; the residual's gradient is dy itself.  dx may be dy. */
+int switch_moe_dropout_bwd(const switch_moe_dropout_config* cfg, const void* dy, const uint64_t* rng, void* dx,
+                           void* stream);
+
+/* The load-balancing loss (Eq. 4-6) of any router: of its own choices or given ones, of one or several choices a token,
+ * with padded tokens left out.  For each of the groups (T / groups consecutive rows)
+ *   p = softmax(logits),  f_i = choices of expert i / (k n),  P_i = sum_t p[t,i] / n,  n = tokens that count,
+ *   loss = mean over groups of alpha E sum_i f_i P_i      (0 for a group with n = 0). */
+typedef struct switch_moe_balance_config {
+  int32_t T, E;              /* tokens, experts (1 <= E <= 1024); T = 0 is an empty call: loss 0 */
+  int32_t k;                 /* choices per token, 1 <= k <= min(E, 16) */
+  int32_t groups;            /* 0 or 1: one; T is a multiple of it; at most 65535 */
+  int32_t dtype;             /* switch_moe_dtype of logits and dlogits */
+  int32_t ld;                /* elements between rows of logits and dlogits; 0: E.  Any distance */
+  float alpha;
+  int32_t reserved[2];       /* must be 0 */
+} switch_moe_balance_config;
+
+/* HOST call.  Bytes of device workspace (1024-byte aligned) of switch_moe_balance_fwd; nothing in it survives a call. */
+int switch_moe_balance_workspace_bytes(const switch_moe_balance_config* cfg, size_t* bytes_out);
+
+/* logits [T,E]; expert_index int32[T,k]: the choices, an entry below 0 or from E on is none; NULL: the k largest logits
+ * of each row, ties to the lowest index, never a NaN or -infinity.  token_mask uint8[T]: 0 = the token does not count,
+ * whatever its row holds; NULL: all do.  A row whose logits are all -infinity does not count either.
+ * loss float[1], counts int32[groups,E], tokens int32[groups] (n of each group): out.  Sums run in a fixed order. */
+int switch_moe_balance_fwd(const switch_moe_balance_config* cfg, const void* logits, const int32_t* expert_index,
+                           const uint8_t* token_mask, float* loss, int32_t* counts, int32_t* tokens, void* workspace,
+                           size_t workspace_bytes, void* stream);
+/* dlogits [T,E] (out; zeros for tokens that do not count) for the upstream gradient d_loss, from the counts and tokens of
+ * the forward call; f carries no gradient (Section 2.2).  dlogits may be logits. */
+int switch_moe_balance_bwd(const switch_moe_balance_config* cfg, const void* logits, const uint8_t* token_mask,
+                           const int32_t* counts, const int32_t* tokens, float d_loss, void* dlogits, void* stream);
+
 /* HOST call.  Static description of a status code. */
 const char* switch_moe_status_string(int status);
 

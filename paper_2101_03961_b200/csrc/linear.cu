@@ -1,0 +1,432 @@
+// The dense layer's entry points (switch_moe_linear_*): argument checks, workspace, launch sequences, and the kernels
+// around the products: dz = dropout(dy) . activation'(pre) with the bias gradient's sums, the bfloat16 parts of float32
+// operands, the sum of a split contraction's parts.
+#include <cstring>
+
+#include "linear_common.cuh"
+
+namespace swmoe {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kColsPerBlock = 256, kRowLanes = 8;    // 32 threads x 8 columns, 8 rows at a time
+
+struct LinearShape {
+  int M, K, N, act, q, site;
+  bool f32;
+  long long ldx, ldw, ldy, elt;
+  long long ldn, ldk;                                // rows of N or K elements in the workspace, multiples of 8
+  int chunks, chunk_rows;                            // row chunks of the dz kernel
+  int dw_splits;
+};
+struct LinearPlan {
+  size_t status, x_parts, w_parts, dz, dz_parts, db_part, dw_part, fwd_total, total;
+};
+
+int resolve(const switch_moe_linear_config* cfg, LinearShape* s) {
+  if (cfg == nullptr) return SWITCH_MOE_INVALID_ARGUMENT;
+  const switch_moe_linear_config& c = *cfg;
+  if (c.M < 0 || c.K <= 0 || c.N <= 0 || c.ldx < 0 || c.ldw < 0 || c.ldy < 0 || c.reserved[0] != 0 || c.reserved[1] != 0)
+    return SWITCH_MOE_INVALID_ARGUMENT;
+  if ((c.ldx > 0 && c.ldx < c.K) || (c.ldw > 0 && c.ldw < c.N) || (c.ldy > 0 && c.ldy < c.N)) return SWITCH_MOE_INVALID_ARGUMENT;
+  if (c.dtype != SWITCH_MOE_BF16 && c.dtype != SWITCH_MOE_F32) return SWITCH_MOE_INVALID_ARGUMENT;
+  if (c.activation < SWITCH_MOE_ACT_NONE || c.activation > SWITCH_MOE_ACT_GELU) return SWITCH_MOE_INVALID_ARGUMENT;
+  s->q = dropout_threshold(c.dropout);
+  if (s->q < 0 || c.site < 0 || c.site > 65535) return SWITCH_MOE_INVALID_ARGUMENT;
+  s->M = c.M; s->K = c.K; s->N = c.N; s->act = c.activation; s->site = c.site;
+  s->f32 = c.dtype == SWITCH_MOE_F32;
+  s->elt = s->f32 ? 4 : 2;
+  s->ldx = c.ldx > 0 ? c.ldx : c.K;
+  s->ldw = c.ldw > 0 ? c.ldw : c.N;
+  s->ldy = c.ldy > 0 ? c.ldy : c.N;
+  if (s->ldx * s->elt % 16 != 0 || s->ldw * s->elt % 16 != 0 || s->ldy * s->elt % 16 != 0) return SWITCH_MOE_UNSUPPORTED_SHAPE;
+  s->ldn = ((long long)c.N + 7) / 8 * 8;
+  s->ldk = ((long long)c.K + 7) / 8 * 8;
+  if ((long long)c.M * (s->ldn / 8) >= 1ll << 48) return SWITCH_MOE_UNSUPPORTED_SHAPE;
+  // about eight blocks per SM, each with at least 32 rows
+  const long long col_blocks = ((long long)c.N + kColsPerBlock - 1) / kColsPerBlock;
+  long long chunks = (8ll * kChipSms + col_blocks - 1) / col_blocks, most = ((long long)c.M + 31) / 32;
+  if (chunks > most) chunks = most;
+  if (chunks < 1) chunks = 1;
+  long long rows = ((long long)c.M + chunks - 1) / chunks;
+  rows = (rows + kRowLanes - 1) / kRowLanes * kRowLanes;
+  if (rows < kRowLanes) rows = kRowLanes;
+  s->chunk_rows = (int)rows;
+  s->chunks = (int)(((long long)c.M + rows - 1) / rows);
+  if (s->chunks > 65535 || col_blocks > 0x7fffffffll) return SWITCH_MOE_UNSUPPORTED_SHAPE;
+  s->dw_splits = dense_splits(c.K, c.N, c.M);
+  return SWITCH_MOE_OK;
+}
+
+void make_plan(const LinearShape& s, LinearPlan* p) {
+  size_t off = 0;
+  auto take = [&](size_t bytes) { size_t o = off; off = (off + bytes + 1023) / 1024 * 1024; return o; };
+  const size_t M = s.M, K = s.K;
+  p->status = take(kStatusWords * 4);
+  p->x_parts = take(s.f32 ? 3 * M * s.ldk * 2 : 0);
+  p->w_parts = take(s.f32 ? 3 * K * s.ldn * 2 : 0);
+  p->fwd_total = off;
+  const bool own_dz = s.act != SWITCH_MOE_ACT_NONE || s.q > 0;
+  p->dz = take(own_dz ? M * s.ldn * s.elt : 0);
+  p->dz_parts = take(s.f32 ? 3 * M * s.ldn * 2 : 0);
+  p->db_part = take((size_t)s.chunks * s.ldn * 4);
+  p->dw_part = take(s.dw_splits > 1 ? (size_t)s.dw_splits * K * s.ldn * 4 : 0);
+  p->total = off;
+}
+
+// Eight consecutive elements of a row, the first `n` of them inside; 16-byte aligned.
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, int n, float* f) {
+  if (n >= 8) {
+    const uint4 v = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = i < n ? __bfloat162float(p[i]) : 0.f;
+  }
+}
+__device__ __forceinline__ void load8(const float* p, int n, float* f) {
+  if (n >= 8) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float4 v = *reinterpret_cast<const float4*>(p + 4 * i);
+      f[4 * i] = v.x; f[4 * i + 1] = v.y; f[4 * i + 2] = v.z; f[4 * i + 3] = v.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = i < n ? p[i] : 0.f;
+  }
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, int n, const float* f) {
+  if (n >= 8) {
+    uint4 v;
+    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+    *reinterpret_cast<uint4*>(p) = v;
+  } else {
+    for (int i = 0; i < n; ++i) p[i] = __float2bfloat16(f[i]);
+  }
+}
+__device__ __forceinline__ void store8(float* p, int n, const float* f) {
+  if (n >= 8) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      *reinterpret_cast<float4*>(p + 4 * i) = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+  } else {
+    for (int i = 0; i < n; ++i) p[i] = f[i];
+  }
+}
+// x 2^24 = h + m + l: three arrays `plane` elements apart.  (A value beyond the parts' range makes m NaN, and with it the
+// results that it meets, which the product then forms again.)
+__device__ __forceinline__ void store_parts8(__nv_bfloat16* p, long long plane, const float* f) {
+  float h[8], m[8], l[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float x = f[i] * kPartUp;
+    h[i] = __bfloat162float(__float2bfloat16(x));
+    const float rest = x - h[i];
+    m[i] = __bfloat162float(__float2bfloat16(rest));
+    l[i] = rest - m[i];
+  }
+  store8(p, 8, h);
+  store8(p + plane, 8, m);
+  store8(p + 2 * plane, 8, l);
+}
+
+// dz and the bias gradient.  A block takes 256 columns of a chunk of rows: 32 threads x 8 columns, 8 rows at a time; its
+// column sums go to `part`, from where they are added up in chunk order.
+struct DzArgs {
+  int M, N, act, chunk_rows, per_row;
+  long long ldy, ldn;
+  DropoutParams dropout;
+};
+template <typename ET>
+__global__ void __launch_bounds__(kThreads)
+linear_dz_kernel(const ET* __restrict__ dy, const ET* __restrict__ pre, DzArgs a, ET* dz, __nv_bfloat16* parts, float* part, int* status) {
+  pdl_launch_dependents();
+  pdl_wait();
+  __shared__ float sums[kRowLanes][kColsPerBlock];
+  if (status != nullptr && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < kStatusWords) status[threadIdx.x] = 0;
+  const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5;
+  const long long col = (long long)blockIdx.x * kColsPerBlock + cx * 8;
+  const int n = (int)(col < a.N ? (a.N - col < 8 ? a.N - col : 8) : 0);
+  const DropoutState rng = dropout_state(a.dropout);
+  float acc[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+  const long long row_end = min((long long)a.M, (long long)(blockIdx.y + 1) * a.chunk_rows);
+  if (n > 0) {
+#pragma unroll 2
+    for (long long row = (long long)blockIdx.y * a.chunk_rows + ry; row < row_end; row += kRowLanes) {
+      float g[8], z[8];
+      load8(dy + row * a.ldy + col, n, g);
+      if (a.act != SWITCH_MOE_ACT_NONE) load8(pre + row * a.ldy + col, n, z);
+      if (a.dropout.rng != nullptr) {
+        const uint4 bits = dropout_bits(a.dropout, rng, (unsigned long long)row * (unsigned)a.per_row + (unsigned)(col >> 3));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float f = dropout_factor(a.dropout, bits, i);
+          g[i] = f != 0.f ? g[i] * f : 0.f;
+        }
+      }
+      if (a.act == SWITCH_MOE_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[i] = z[i] > 0.f ? g[i] : 0.f;
+      } else if (a.act == SWITCH_MOE_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[i] *= activation_derivative(SWITCH_MOE_ACT_GELU, z[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[i] += g[i];
+      if (dz != nullptr) store8(dz + row * a.ldn + col, 8, g);          // (the workspace's rows are multiples of 8)
+      if (parts != nullptr) store_parts8(parts + row * a.ldn + col, (long long)a.M * a.ldn, g);
+    }
+  }
+  if (part == nullptr) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sums[ry][cx * 8 + i] = acc[i];
+  __syncthreads();
+  float s = 0.f;
+#pragma unroll
+  for (int r = 0; r < kRowLanes; ++r) s += sums[r][threadIdx.x];
+  const long long c = (long long)blockIdx.x * kColsPerBlock + threadIdx.x;
+  if (c < a.N) part[(long long)blockIdx.y * a.ldn + c] = s;
+}
+
+// db[c] = sum over chunks: 32 columns per block, 8 chunks at a time.
+__global__ void __launch_bounds__(kThreads)
+linear_db_kernel(const float* __restrict__ part, int chunks, int N, long long ldn, float* db) {
+  pdl_launch_dependents();
+  pdl_wait();
+  __shared__ float sums[8][32];
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const long long c = (long long)blockIdx.x * 32 + lane;
+  float s = 0.f;
+  if (c < N)
+    for (int i = w; i < chunks; i += 8) s += part[(long long)i * ldn + c];
+  sums[w][lane] = s;
+  __syncthreads();
+  if (w == 0 && c < N) {
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += sums[i][lane];
+    db[c] = s;
+  }
+}
+
+// The parts of a float32 matrix, eight elements of a row per thread.
+__global__ void __launch_bounds__(kThreads)
+linear_parts_kernel(const float* __restrict__ src, long long ld, long long rows, int cols, long long ld_out, __nv_bfloat16* parts) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const long long per_row = ld_out / 8, total = rows * per_row;
+  for (long long b = (long long)blockIdx.x * kThreads + threadIdx.x; b < total; b += (long long)gridDim.x * kThreads) {
+    const long long row = b / per_row;
+    const int col = (int)(b - row * per_row) * 8;
+    float f[8];
+    load8(src + row * ld + col, cols - col, f);
+    store_parts8(parts + row * ld_out + col, rows * ld_out, f);
+  }
+}
+
+// out = sum of the parts, in order.
+template <typename ET>
+__global__ void __launch_bounds__(kThreads)
+linear_add_kernel(const float* __restrict__ part, int splits, long long rows, int cols, long long ld_part, ET* out, long long ld_out) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const long long per_row = ld_part / 8, total = rows * per_row;
+  for (long long b = (long long)blockIdx.x * kThreads + threadIdx.x; b < total; b += (long long)gridDim.x * kThreads) {
+    const long long row = b / per_row;
+    const int col = (int)(b - row * per_row) * 8;
+    const int n = cols - col < 8 ? cols - col : 8;
+    float s[8];
+    load8(part + row * ld_part + col, n, s);
+    for (int i = 1; i < splits; ++i) {
+      float f[8];
+      load8(part + ((long long)i * rows + row) * ld_part + col, n, f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[j] += f[j];
+    }
+    store8(out + row * ld_out + col, n, s);
+  }
+}
+
+unsigned flat_grid(long long threads) {
+  const long long want = (threads + kThreads - 1) / kThreads, most = 16ll * kChipSms;
+  return (unsigned)(want < most ? want : most);
+}
+
+int launch_parts(const void* src, long long ld, long long rows, int cols, long long ld_out, __nv_bfloat16* parts, cudaStream_t st) {
+  launch_k(linear_parts_kernel, dim3(flat_grid(rows * (ld_out / 8))), dim3(kThreads), 0, st, static_cast<const float*>(src), ld,
+           rows, cols, ld_out, parts);
+  return launch_status();
+}
+
+template <typename ET>
+int launch_dz(const LinearShape& s, const void* dy, const void* pre, const uint64_t* rng, void* dz, __nv_bfloat16* parts,
+              float* part, int* status, cudaStream_t st) {
+  DzArgs a{s.M, s.N, s.act, s.chunk_rows, (int)(s.ldn / 8), s.ldy, s.ldn, dropout_params(rng, s.q, s.site)};
+  launch_k(linear_dz_kernel<ET>, dim3((unsigned)((s.N + kColsPerBlock - 1) / kColsPerBlock), s.chunks), dim3(kThreads), 0, st,
+           static_cast<const ET*>(dy), static_cast<const ET*>(pre), a, static_cast<ET*>(dz), parts, part, status);
+  return launch_status();
+}
+
+int check_workspace(const void* workspace, size_t have, size_t need) {
+  if (workspace == nullptr) return SWITCH_MOE_INVALID_ARGUMENT;
+  if ((reinterpret_cast<uintptr_t>(workspace) & 1023u) != 0) return SWITCH_MOE_UNSUPPORTED_SHAPE;
+  return have < need ? SWITCH_MOE_WORKSPACE_TOO_SMALL : SWITCH_MOE_OK;
+}
+
+#define SWMOE_TRY(expr)                    \
+  do {                                     \
+    int rc__ = (expr);                     \
+    if (rc__ != SWITCH_MOE_OK) return rc__; \
+  } while (0)
+
+}  // namespace
+}  // namespace swmoe
+
+using namespace swmoe;
+
+extern "C" int switch_moe_linear_workspace_bytes(const switch_moe_linear_config* cfg, int32_t backward, size_t* bytes_out) {
+  if (bytes_out == nullptr) return SWITCH_MOE_INVALID_ARGUMENT;
+  LinearShape s;
+  SWMOE_TRY(resolve(cfg, &s));
+  LinearPlan p;
+  make_plan(s, &p);
+  *bytes_out = backward != 0 ? p.total : p.fwd_total;
+  return SWITCH_MOE_OK;
+}
+
+extern "C" int switch_moe_linear_fwd(const switch_moe_linear_config* cfg, const void* x, const void* W, const float* bias,
+                                     const void* residual, const uint64_t* rng, void* y, void* pre, void* workspace,
+                                     size_t workspace_bytes, void* stream) {
+  LinearShape s;
+  SWMOE_TRY(resolve(cfg, &s));
+  LinearPlan p;
+  make_plan(s, &p);
+  SWMOE_TRY(check_workspace(workspace, workspace_bytes, p.fwd_total));
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int* status = ws_ptr<int>(workspace, p.status);
+  if (s.M == 0)
+    return cudaMemsetAsync(status, 0, kStatusWords * 4, st) == cudaSuccess ? SWITCH_MOE_OK : SWITCH_MOE_CUDA_ERROR;
+  if (x == nullptr || W == nullptr || y == nullptr || (s.q > 0 && rng == nullptr)) return SWITCH_MOE_INVALID_ARGUMENT;
+  if (!aligned16(x) || !aligned16(W) || !aligned16(y) || !aligned16(pre) || !aligned16(residual) || !aligned16(bias) ||
+      (reinterpret_cast<uintptr_t>(rng) & 7u) != 0)
+    return SWITCH_MOE_UNSUPPORTED_SHAPE;
+  DenseProduct q{};
+  q.rows = s.M; q.cols = s.N; q.k = s.K; q.f32 = s.f32; q.splits = 1;
+  q.a = {x, s.ldx, static_cast<const float*>(x), s.ldx, 1};
+  q.b = {W, s.ldw, static_cast<const float*>(W), 1, s.ldw};
+  q.out = y; q.ld_out = s.ldy; q.status = status; q.clear_status = true;
+  if (s.f32) {
+    __nv_bfloat16* xp = ws_ptr<__nv_bfloat16>(workspace, p.x_parts);
+    __nv_bfloat16* wp = ws_ptr<__nv_bfloat16>(workspace, p.w_parts);
+    SWMOE_TRY(launch_parts(x, s.ldx, s.M, s.K, s.ldk, xp, st));
+    SWMOE_TRY(launch_parts(W, s.ldw, s.K, s.N, s.ldn, wp, st));
+    q.a.p = xp; q.a.ld = s.ldk;
+    q.b.p = wp; q.b.ld = s.ldn;
+  }
+  const DenseEpilogue e{bias, residual, pre, s.act, (int)(s.ldn / 8), dropout_params(rng, s.q, s.site)};
+  return launch_dense(kDenseFwd, q, e, st);
+}
+
+extern "C" int switch_moe_linear_bwd(const switch_moe_linear_config* cfg, const void* dy, const void* x, const void* W,
+                                     const void* pre, const uint64_t* rng, void* workspace, size_t workspace_bytes,
+                                     void* dx, void* dW, float* dbias, void* stream) {
+  LinearShape s;
+  SWMOE_TRY(resolve(cfg, &s));
+  LinearPlan p;
+  make_plan(s, &p);
+  SWMOE_TRY(check_workspace(workspace, workspace_bytes, p.total));
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (!aligned16(dy) || !aligned16(x) || !aligned16(W) || !aligned16(pre) || !aligned16(dx) || !aligned16(dW) ||
+      !aligned16(dbias) || (reinterpret_cast<uintptr_t>(rng) & 7u) != 0)
+    return SWITCH_MOE_UNSUPPORTED_SHAPE;
+  int* status = ws_ptr<int>(workspace, p.status);
+  if (s.M == 0) {
+    if (cudaMemsetAsync(status, 0, kStatusWords * 4, st) != cudaSuccess) return SWITCH_MOE_CUDA_ERROR;
+    if (dW != nullptr && cudaMemset2DAsync(dW, s.ldw * s.elt, 0, s.N * s.elt, s.K, st) != cudaSuccess) return SWITCH_MOE_CUDA_ERROR;
+    if (dbias != nullptr && cudaMemsetAsync(dbias, 0, (size_t)s.N * 4, st) != cudaSuccess) return SWITCH_MOE_CUDA_ERROR;
+    return SWITCH_MOE_OK;
+  }
+  if (dy == nullptr || (dW != nullptr && x == nullptr) || (dx != nullptr && W == nullptr) ||
+      (s.act != SWITCH_MOE_ACT_NONE && pre == nullptr) || (s.q > 0 && rng == nullptr))
+    return SWITCH_MOE_INVALID_ARGUMENT;
+  const bool products = dx != nullptr || dW != nullptr, own_dz = s.act != SWITCH_MOE_ACT_NONE || s.q > 0;
+  bool cleared = false;
+  void* dz = own_dz && products ? ws_ptr<void>(workspace, p.dz) : nullptr;
+  __nv_bfloat16* dz_parts = s.f32 && products ? ws_ptr<__nv_bfloat16>(workspace, p.dz_parts) : nullptr;
+  float* db_part = dbias != nullptr ? ws_ptr<float>(workspace, p.db_part) : nullptr;
+  if (dz != nullptr || dz_parts != nullptr || db_part != nullptr) {
+    SWMOE_TRY(s.f32 ? launch_dz<float>(s, dy, pre, rng, dz, dz_parts, db_part, status, st)
+                    : launch_dz<__nv_bfloat16>(s, dy, pre, rng, dz, dz_parts, db_part, status, st));
+    cleared = true;
+  }
+  if (dbias != nullptr) {
+    launch_k(linear_db_kernel, dim3((unsigned)((s.N + 31) / 32)), dim3(kThreads), 0, st, static_cast<const float*>(db_part),
+             s.chunks, s.N, s.ldn, dbias);
+    SWMOE_TRY(launch_status());
+  }
+  const void* g = dz != nullptr ? dz : dy;
+  const long long ldg = dz != nullptr ? s.ldn : s.ldy;
+  DenseOperand go{s.f32 ? dz_parts : g, s.f32 ? s.ldn : ldg, static_cast<const float*>(g), 0, 0};
+  if (dx != nullptr) {
+    DenseProduct q{};
+    q.rows = s.M; q.cols = s.K; q.k = s.N; q.f32 = s.f32; q.splits = 1;
+    q.a = go; q.a.si = ldg; q.a.sk = 1;
+    q.b = {W, s.ldw, static_cast<const float*>(W), s.ldw, 1};
+    if (s.f32) {
+      __nv_bfloat16* wp = ws_ptr<__nv_bfloat16>(workspace, p.w_parts);
+      SWMOE_TRY(launch_parts(W, s.ldw, s.K, s.N, s.ldn, wp, st));
+      q.b.p = wp; q.b.ld = s.ldn;
+    }
+    q.out = dx; q.ld_out = s.ldx; q.status = status; q.clear_status = !cleared;
+    SWMOE_TRY(launch_dense(kDenseDx, q, DenseEpilogue{}, st));
+    cleared = true;
+  }
+  if (dW != nullptr) {
+    DenseProduct q{};
+    q.rows = s.K; q.cols = s.N; q.k = s.M; q.f32 = s.f32; q.splits = s.dw_splits;
+    q.a = {x, s.ldx, static_cast<const float*>(x), 1, s.ldx};
+    q.b = go; q.b.si = 1; q.b.sk = ldg;
+    if (s.f32) {
+      __nv_bfloat16* xp = ws_ptr<__nv_bfloat16>(workspace, p.x_parts);
+      SWMOE_TRY(launch_parts(x, s.ldx, s.M, s.K, s.ldk, xp, st));
+      q.a.p = xp; q.a.ld = s.ldk;
+    }
+    q.status = status; q.clear_status = !cleared;
+    float* part = ws_ptr<float>(workspace, p.dw_part);
+    q.out = s.dw_splits > 1 ? part : dW;
+    q.ld_out = s.dw_splits > 1 ? s.ldn : s.ldw;
+    SWMOE_TRY(launch_dense(kDenseDw, q, DenseEpilogue{}, st));
+    if (s.dw_splits > 1) {
+      const dim3 grid(flat_grid((long long)s.K * (s.ldn / 8)));
+      const float* cp = part;
+      if (s.f32)
+        launch_k(linear_add_kernel<float>, grid, dim3(kThreads), 0, st, cp, s.dw_splits, (long long)s.K, s.N, s.ldn,
+                 static_cast<float*>(dW), s.ldw);
+      else
+        launch_k(linear_add_kernel<__nv_bfloat16>, grid, dim3(kThreads), 0, st, cp, s.dw_splits, (long long)s.K, s.N, s.ldn,
+                 static_cast<__nv_bfloat16*>(dW), s.ldw);
+      SWMOE_TRY(launch_status());
+    }
+  }
+  return SWITCH_MOE_OK;
+}
+
+extern "C" int switch_moe_linear_check_device_status(const switch_moe_linear_config* cfg, void* workspace,
+                                                     int32_t* info_out, void* stream) {
+  LinearShape s;
+  SWMOE_TRY(resolve(cfg, &s));
+  SWMOE_TRY(check_workspace(workspace, ~(size_t)0, 0));
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int32_t host[kStatusWords];
+  if (cudaMemcpyAsync(host, workspace, sizeof(host), cudaMemcpyDeviceToHost, st) != cudaSuccess) return SWITCH_MOE_CUDA_ERROR;
+  if (cudaStreamSynchronize(st) != cudaSuccess) return SWITCH_MOE_CUDA_ERROR;
+  if (info_out != nullptr) std::memcpy(info_out, host, sizeof(host));
+  return host[0] != 0 ? SWITCH_MOE_DEVICE_TIMEOUT : SWITCH_MOE_OK;
+}

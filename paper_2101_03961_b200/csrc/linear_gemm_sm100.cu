@@ -1,0 +1,607 @@
+// The products of the dense layer on pairs of SMs (tcgen05 cta_group::2, M = 256): y = x W with bias, activation, dropout
+// and residual in its epilogue, dx = dz W^T, dW = x^T dz.
+//
+// A CTA pair works on tiles of 256 x TN outputs (TN 256, or 128 where that fills the chip better); each CTA stages its own
+// 128 rows of A and half of B's columns per 64-deep block of the contraction by TMA, the leader's MMA warp issues the
+// instructions for both, and eight epilogue warps of each CTA drain its 128 accumulator lanes (a lane = an output row)
+// while the next tile's products run in the other half of tensor memory.  Four of them form a group that takes every
+// second chunk of 128 bytes of the output rows: from tensor memory through the epilogue into 128-byte-swizzled shared
+// memory, and from there by TMA, which also brings the residual's chunk into the very buffer that the result leaves from
+// and clips what is outside (a store in whole 16-byte pieces: the last columns of a row that does not end on one are
+// written element by element).
+//
+// Float32 operands come as three bfloat16 parts (x 2^24 = h + m + l, exact); of the nine cross products six are formed,
+// the others are below 2^-25 of the product.  The tensor pipe adds with truncation, so an accumulator lives for one block
+// of 64 steps only (the corrections first, h.h last) and is then added to a float32 sum in registers, round to nearest.
+// Results that are not finite are formed again by fused multiply-adds from the float32 operands (operands from 2^104 on
+// and sums from 2^80 on end there too).
+//
+// Every wait is bounded in time; after one gave up all roles leave, and the threads of an epilogue group decide together.
+#include <cmath>
+
+#include "linear_common.cuh"
+#include "tc_common.cuh"
+
+namespace swmoe {
+using namespace tc;
+namespace {
+
+constexpr int kThreads = 320;                        // TMA, MMA, eight epilogue warps
+constexpr int kABlock = 16384;                       // 128 rows x 64 steps of bfloat16
+constexpr int kChunkBytes = 16384;                   // 128 rows x 128 bytes of output
+constexpr int kBuffers = 2;                          // chunks in shared memory per epilogue group
+constexpr int kStagingBytes = 2 * kBuffers * kChunkBytes;
+constexpr int kRingBytes = 163840;
+constexpr int kMaxRing = 8;
+constexpr int kBiasBytes = 2 * 64 * 4;
+constexpr int kSmem = 1024 + kRingBytes + kStagingBytes + kBiasBytes + 256;
+constexpr uint32_t kPeer = 0xFEFFFFFFu;              // clears the CTA-rank bit of a shared::cluster address
+constexpr int kBand = 8;                             // row tiles that are walked together along the columns
+
+enum Mode { kBf16 = 0, kPartial = 1, kF32 = 2 };     // bf16 -> bf16; bf16 -> float32 part sums; float32 parts -> float32
+
+struct DenseParams {
+  int rows, cols, k_blocks;
+  int m_tiles, n_tiles, splits, k_per_split;
+  long long k;
+  int activation, dropout_blocks;
+  int has_residual, has_pre;
+  const float* bias;
+  DropoutParams dropout;
+  const float* a; long long a_si, a_sk;
+  const float* b; long long b_si, b_sk;
+  int whole_cols;                                    // columns in whole 16-byte pieces: a TMA store clips at these, the rest
+  void* out; void* pre; long long ld_out, split_out; // of a row is written by the threads themselves
+  int* status;
+  int clear_status;
+};
+
+struct DenseMaps {
+  CUtensorMap a, b, out, pre, residual;
+};
+
+__device__ __forceinline__ uint32_t cta_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void arrive_at(uint32_t local_bar, uint32_t cta) {
+  asm volatile(
+      "{\n\t.reg .b32 ra;\n\t"
+      "mapa.shared::cluster.u32 ra, %0, %1;\n\t"
+      "mbarrier.arrive.shared::cluster.b64 _, [ra];\n\t}" ::"r"(local_bar), "r"(cta) : "memory");
+}
+__device__ __forceinline__ void store_at(uint32_t local, uint32_t cta, uint32_t v) {
+  asm volatile(
+      "{\n\t.reg .b32 ra;\n\t"
+      "mapa.shared::cluster.u32 ra, %0, %1;\n\t"
+      "st.volatile.shared::cluster.u32 [ra], %2;\n\t}" ::"r"(local), "r"(cta), "r"(v) : "memory");
+}
+__device__ __forceinline__ void load_pair(uint32_t dst, const CUtensorMap* tm, uint32_t leader_bar, int c0, int c1, int c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(leader_bar), "r"(c0), "r"(c1),
+      "r"(c2) : "memory");
+}
+__device__ __forceinline__ void store_box(const CUtensorMap* tm, uint32_t src, int c0, int c1, int c2) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(
+                   reinterpret_cast<uint64_t>(tm)), "r"(src), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+__device__ __forceinline__ void commit_pair(uint32_t bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+      "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Barrier of one epilogue group (128 threads); true if `ok` holds in every one of them.
+__device__ __forceinline__ bool group_all(int group, bool ok) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %2, 0;\n\t"
+      "barrier.cta.red.and.pred q, %1, 128, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(group + 1), "r"((uint32_t)ok) : "memory");
+  return r != 0;
+}
+// Registers pass through so that no use of them moves ahead of the wait.
+__device__ __forceinline__ void wait_ld(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+                 "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+                 "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+               :: "memory");
+}
+__device__ __forceinline__ uint32_t pack2_bf16(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// The columns of a piece of eight that belong to no whole 16 bytes of the row.
+template <bool kOut4>
+__device__ __forceinline__ void store_ragged(const DenseParams& p, void* base, long long at, int col, const float* x) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (col + i >= p.whole_cols && col + i < p.cols) {
+      if (kOut4) static_cast<float*>(base)[at + i] = x[i];
+      else static_cast<__nv_bfloat16*>(base)[at + i] = __float2bfloat16(x[i]);
+    }
+}
+
+struct Unit {
+  int m0, n0, split, kb0, kb1;
+};
+// Bands of kBand row tiles, walked column by column, so that what runs at one time shares rows of A and columns of B.
+__device__ __forceinline__ Unit decode(const DenseParams& p, int id, int TN) {
+  Unit u;
+  const int tiles = p.m_tiles * p.n_tiles;
+  u.split = id / tiles;
+  const int t = id - u.split * tiles, per_band = kBand * p.n_tiles, band = t / per_band, r = t - band * per_band;
+  const int height = min(kBand, p.m_tiles - band * kBand), n = r / height;
+  u.m0 = (band * kBand + r - n * height) * 256;
+  u.n0 = n * TN;
+  u.kb0 = u.split * p.k_per_split;
+  u.kb1 = min(p.k_blocks, u.kb0 + p.k_per_split);
+  return u;
+}
+
+// Float32: which parts are multiplied, from the smallest products up (2 bits each): h.l, l.h, m.m, h.m, m.h, h.h.
+__device__ __forceinline__ int part_a(int q) { return (0x0118u >> (2 * q)) & 3; }   // 0, 2, 1, 0, 1, 0
+__device__ __forceinline__ int part_b(int q) { return (0x0052u >> (2 * q)) & 3; }   // 2, 0, 1, 1, 0, 0
+
+template <bool kAMn, bool kBMn, int TN, int kMode>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant__ DenseParams p) {
+  constexpr bool kFwd = !kAMn && kBMn;                       // the only product with an epilogue of its own
+  constexpr bool kOut4 = kMode != kBf16;                     // float32 output
+  constexpr int kChunk = kOut4 ? 32 : 64;                    // output columns per chunk
+  constexpr int kBBlock = TN * 64;                           // this CTA's half of B: TN / 2 columns x 64 steps
+  constexpr int kStage = kABlock + kBBlock;
+  constexpr int kStages = kRingBytes / kStage < kMaxRing ? kRingBytes / kStage : kMaxRing;
+  constexpr int kParts = kMode == kF32 ? 6 : 1;
+  pdl_launch_dependents();
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
+  float* bias_s = reinterpret_cast<float*>(gen + kRingBytes + kStagingBytes);
+  uint8_t* bar_gen = gen + kRingBytes + kStagingBytes + kBiasBytes;
+  const uint32_t bars = base + kRingBytes + kStagingBytes + kBiasBytes;
+  // full[8] | empty[8] | acc_full[2] | acc_empty[2] | residual[2 groups x 2] | tmem | abort, progress
+  const uint32_t full0 = bars, empty0 = bars + 64u, afull0 = bars + 128u, aempty0 = bars + 144u, res0 = bars + 160u;
+  volatile uint32_t* tmem_s = reinterpret_cast<volatile uint32_t*>(bar_gen + 192);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bar_gen + 200);
+  const int warp = uniform_warp_id(), lane = threadIdx.x & 31;
+  const uint32_t rank = __shfl_sync(0xffffffffu, cta_rank(), 0);
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kMaxRing; ++s) { mbar_init(full0 + 8u * s, 1); mbar_init(empty0 + 8u * s, 1); }
+    for (int a = 0; a < 2; ++a) { mbar_init(afull0 + 8u * a, 1); mbar_init(aempty0 + 8u * a, 16); }
+    for (int a = 0; a < 4; ++a) mbar_init(res0 + 8u * a, 1);
+    abort_flag[0] = 0;
+    abort_flag[1] = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                     smem_u32(const_cast<uint32_t*>(tmem_s))), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  pdl_wait();
+  if (p.clear_status && blockIdx.x == 0 && threadIdx.x < kStatusWords) p.status[threadIdx.x] = 0;
+  tc_fence_before();
+  cluster_sync();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_s;
+  const int n_units = p.m_tiles * p.n_tiles * p.splits, pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  constexpr bool kProgress = kMode == kF32;                  // redone results take their time
+
+  if (warp == 0) {
+    // ------------------------------------------------------------------------------------------ loads (both CTAs)
+    uint32_t stage = 0, phase = 0;
+    bool ok = true;
+    for (int id = pair; id < n_units && ok; id += n_pairs) {
+      const Unit u = decode(p, id, TN);
+      const int am = u.m0 + 128 * (int)rank, bn = u.n0 + TN / 2 * (int)rank;
+#pragma unroll 1
+      for (int kb = u.kb0; kb < u.kb1 && ok; ++kb) {
+#pragma unroll 1
+        for (int q = 0; q < kParts; ++q) {
+          const int pa = kParts > 1 ? part_a(q) : 0, pb = kParts > 1 ? part_b(q) : 0;
+          ok = mbar_wait_warp<kProgress>(empty0 + 8u * stage, phase ^ 1u, abort_flag, p.status, 41);
+          if (!ok) break;
+          const uint32_t a_dst = base + stage * kStage, b_dst = a_dst + kABlock, fb = full0 + 8u * stage;
+          const uint32_t lead = fb & kPeer;                  // both CTAs' bytes count on the leader's barrier
+          const int k0 = kb * kBK;
+          if (elect_one()) {
+            if (rank == 0) mbar_arrive_expect_tx(fb, 2u * kStage);
+            if (kAMn) {
+              load_pair(a_dst, &maps.a, lead, am, k0, pa);
+              load_pair(a_dst + kAtomBytes, &maps.a, lead, am + 64, k0, pa);
+            } else {
+              load_pair(a_dst, &maps.a, lead, k0, am, pa);
+            }
+            if (kBMn) {
+              load_pair(b_dst, &maps.b, lead, bn, k0, pb);
+              if (TN == 256) load_pair(b_dst + kAtomBytes, &maps.b, lead, bn + 64, k0, pb);
+            } else {
+              load_pair(b_dst, &maps.b, lead, k0, bn, pb);
+            }
+          }
+          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        }
+      }
+    }
+    if (*abort_flag != 0) {
+      const long long t0 = clock64();
+      while (clock64() - t0 < 4000000ll) __nanosleep(1000);  // let copies in flight land (about 2 ms)
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------------------------------ products (leader CTA)
+    if (rank == 0) {
+      constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)kAMn << 15) | ((uint32_t)kBMn << 16) |
+                                 ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(256 >> 4) << 24);
+      constexpr uint32_t a_step = (kAMn ? kUmmaK * 128u : kUmmaK * 2u) >> 4, b_step = (kBMn ? kUmmaK * 128u : kUmmaK * 2u) >> 4;
+      const uint64_t a_desc = make_smem_desc(base, kAMn ? kAtomBytes : 16u, 1024u);
+      const uint64_t b_desc = make_smem_desc(base + kABlock, kBMn ? kAtomBytes : 16u, 1024u);
+      uint32_t stage = 0, phase = 0, it = 0;
+      bool ok = true;
+      for (int id = pair; id < n_units && ok; id += n_pairs) {
+        const Unit u = decode(p, id, TN);
+        uint32_t d = 0;
+#pragma unroll 1
+        for (int kb = u.kb0; kb < u.kb1 && ok; ++kb) {
+          const bool first = kMode == kF32 || kb == u.kb0, done = kMode == kF32 || kb == u.kb1 - 1;
+          const uint32_t side = it & 1u;
+          if (first) {                                       // this half's previous accumulator has been read out
+            ok = mbar_wait_warp<kProgress>(aempty0 + 8u * side, ((it >> 1) & 1u) ^ 1u, abort_flag, p.status, 42);
+            if (!ok) break;
+            tc_fence_after();
+            d = tmem + side * TN;
+          }
+#pragma unroll 1
+          for (int q = 0; q < kParts; ++q) {
+            ok = mbar_wait_warp<kProgress>(full0 + 8u * stage, phase, abort_flag, p.status, 43);
+            if (!ok) break;
+            tc_fence_after();
+            const uint64_t ad = a_desc + (uint64_t)(stage * (kStage >> 4)), bd = b_desc + (uint64_t)(stage * (kStage >> 4));
+            const uint32_t acc = first && q == 0 ? 0u : 1u;
+            if (elect_one()) {
+#pragma unroll
+              for (int ks = 0; ks < kBK / kUmmaK; ++ks)
+                mma_pair(d, ad + ks * a_step, bd + ks * b_step, idesc, ks > 0 ? 1u : acc);
+              commit_pair(empty0 + 8u * stage);
+              if (done && q == kParts - 1) commit_pair(afull0 + 8u * side);
+            }
+            if (++stage == kStages) { stage = 0; phase ^= 1u; }
+          }
+          if (done) ++it;
+        }
+      }
+    }
+  } else {
+    // ------------------------------------------------------------------------------------------ epilogue (both CTAs)
+    const int lg = warp & 3, group = (warp - 2) >> 2, t = (int)threadIdx.x - 64 - 128 * group;   // t: thread of the group
+    const int r = 32 * lg + lane;                            // this thread's row of the CTA's 128
+    const bool boss = t == 0;                                // issues the group's copies
+    const uint32_t stage_s = base + kRingBytes + (uint32_t)(group * kBuffers * kChunkBytes);
+    uint8_t* stage_g = gen + kRingBytes + group * kBuffers * kChunkBytes;
+    float* bias_g = bias_s + 64 * group;
+    const uint32_t row_off = (uint32_t)r * 128u, sw = (uint32_t)(r & 7);
+    const bool pre = kFwd && p.has_pre, residual = kFwd && p.has_residual;
+    DropoutState rng{};
+    if (kFwd) rng = dropout_state(p.dropout);
+    uint32_t it = 0, n_chunk = 0, res_phase = 0;             // res_phase: a bit per buffer
+    bool ok = true;
+    constexpr int kSums = kMode == kF32 ? TN / 2 : 1;
+    for (int id = pair; id < n_units && ok; id += n_pairs) {
+      const Unit u = decode(p, id, TN);
+      const int row0 = u.m0 + 128 * (int)rank;
+      const long long row = row0 + r;
+      float sum[kSums];
+      uint32_t taddr = 0;
+      if constexpr (kMode == kF32) {
+        // a group holds one half of the tile's columns, a chunk of 32 after the other
+#pragma unroll
+        for (int i = 0; i < kSums; ++i) sum[i] = 0.f;
+        for (int kb = u.kb0; kb < u.kb1; ++kb, ++it) {
+          const uint32_t side = it & 1u;
+          ok = mbar_wait_warp<true>(afull0 + 8u * side, (it >> 1) & 1u, abort_flag, p.status, 44);
+          if (!ok) break;
+          tc_fence_after();
+          taddr = tmem + ((uint32_t)(lg * 32) << 16) + side * TN + group * (TN / 2);
+#pragma unroll
+          for (int c = 0; c < TN / 64; ++c) {
+            uint32_t v[32];
+            tc_ld32(taddr + 32u * c, v);
+            wait_ld(v);
+            if (c == TN / 64 - 1) {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) arrive_at(aempty0 + 8u * side, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 32; ++i) sum[32 * c + i] += __uint_as_float(v[i]);
+          }
+        }
+      } else {
+        const uint32_t side = it & 1u;
+        ok = mbar_wait_warp(afull0 + 8u * side, (it >> 1) & 1u, abort_flag, p.status, 44);
+        taddr = tmem + ((uint32_t)(lg * 32) << 16) + side * TN;
+      }
+      if (!group_all(group, ok)) { ok = false; break; }
+      if (kMode != kF32) tc_fence_after();
+      constexpr int kMine = TN / kChunk / 2;                 // chunks of a group
+#pragma unroll
+      for (int c = 0; c < kMine; ++c) {
+        const int chunk = kMode == kF32 ? group * kMine + c : 2 * c + group;
+        const int col0 = u.n0 + chunk * kChunk;
+        const bool inside = col0 < p.cols && row0 < p.rows;  // the same in the whole group
+        uint32_t v[kMode == kBf16 ? 64 : 32];
+        if constexpr (kMode != kF32) {
+          tc_ld32(taddr + (uint32_t)(chunk * kChunk), v);
+          if constexpr (kMode == kBf16) tc_ld32(taddr + (uint32_t)(chunk * kChunk + 32), v + 32);
+        }
+        const uint32_t buf = pre ? 0u : (n_chunk & 1u) * kChunkBytes;
+        if (inside) {
+          if (boss) {                                        // the buffers of this chunk have been read by their last stores
+            if (pre) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            else asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+            if (residual) {
+              const uint32_t rb = res0 + 16u * group + (buf ? 8u : 0u);
+              mbar_arrive_expect_tx(rb, kChunkBytes);
+              tma_load_3d(stage_s + buf, &maps.residual, rb, col0, row0, 0);
+            }
+          }
+          if (kFwd && p.bias != nullptr && t < kChunk) bias_g[t] = col0 + t < p.cols ? p.bias[col0 + t] : 0.f;
+          if (residual) {
+            const uint32_t bit = buf ? 2u : 1u;
+            ok = mbar_wait_warp<kProgress>(res0 + 16u * group + (buf ? 8u : 0u), (res_phase & bit) ? 1u : 0u, abort_flag, p.status, 45);
+            res_phase ^= bit;
+          }
+        }
+        __syncwarp();
+        if constexpr (kMode != kF32) {
+          wait_ld(v);
+          if constexpr (kMode == kBf16) wait_ld(v + 32);
+          if (c == kMine - 1) {                              // the accumulator has been read out
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_at(aempty0 + 8u * (it & 1u), 0);
+          }
+        }
+        if (!inside) continue;
+        if (!group_all(group, ok)) { ok = false; break; }
+        uint8_t* dst = stage_g + buf + row_off;
+#pragma unroll
+        for (int j = 0; j < kChunk / 8; ++j) {
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            if constexpr (kMode == kF32) x[i] = sum[32 * c + 8 * j + i] * kPartDown;
+            else x[i] = __uint_as_float(v[8 * j + i]);
+          }
+          const int col = col0 + 8 * j;
+          const bool ragged = col + 8 > p.whole_cols && col < p.cols && row < p.rows;
+          if constexpr (kMode == kF32) {
+            bool finite = true;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) finite = finite && isfinite(x[i]);
+            if (!finite && row < p.rows) {
+#pragma unroll 1
+              for (int i = 0; i < 8; ++i) {
+                if (col + i >= p.cols) break;
+                float again = 0.f;
+                const float* pa = p.a + row * p.a_si;
+                const float* pb = p.b + (long long)(col + i) * p.b_si;
+                const long long k1 = min(p.k, (long long)u.kb1 * kBK);
+                for (long long k = (long long)u.kb0 * kBK; k < k1; ++k) again = fmaf(pa[k * p.a_sk], pb[k * p.b_sk], again);
+#pragma unroll
+                for (int n = 0; n < 8; ++n)
+                  if (n == i && !isfinite(x[n])) x[n] = again;
+                for (uint32_t cta = 0; cta < 2; ++cta)       // the waiting warps of both CTAs see that work goes on
+                  store_at(bars + 204u, cta, (uint32_t)clock64());
+              }
+            }
+          }
+          if constexpr (kFwd) {
+            if (p.bias != nullptr) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) x[i] += bias_g[8 * j + i];
+            }
+            if (pre) {
+              if (ragged) store_ragged<kOut4>(p, p.pre, row * p.ld_out + col, col, x);
+              uint8_t* pd = stage_g + kChunkBytes + row_off;
+              if constexpr (kOut4) {
+                *reinterpret_cast<float4*>(pd + (((2u * j) ^ sw) << 4)) = make_float4(x[0], x[1], x[2], x[3]);
+                *reinterpret_cast<float4*>(pd + (((2u * j + 1u) ^ sw) << 4)) = make_float4(x[4], x[5], x[6], x[7]);
+              } else {
+                *reinterpret_cast<uint4*>(pd + (((uint32_t)j ^ sw) << 4)) =
+                    make_uint4(pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]), pack2_bf16(x[4], x[5]), pack2_bf16(x[6], x[7]));
+              }
+            }
+            if (p.activation == SWITCH_MOE_ACT_RELU) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) x[i] = x[i] < 0.f ? 0.f : x[i];      // (NaN stays)
+            } else if (p.activation == SWITCH_MOE_ACT_GELU) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) x[i] = gelu_exact(x[i]);
+            }
+            if (p.dropout.rng != nullptr) {
+              const uint4 bits = dropout_bits(p.dropout, rng, (unsigned long long)row * (unsigned)p.dropout_blocks + (unsigned)(col >> 3));
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const float f = dropout_factor(p.dropout, bits, i);
+                x[i] = f != 0.f ? x[i] * f : 0.f;
+              }
+            }
+            if (residual) {
+              if constexpr (kOut4) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                  const float4 f = *reinterpret_cast<const float4*>(dst + (((2u * j + h) ^ sw) << 4));
+                  x[4 * h] += f.x; x[4 * h + 1] += f.y; x[4 * h + 2] += f.z; x[4 * h + 3] += f.w;
+                }
+              } else {
+                const uint4 w = *reinterpret_cast<const uint4*>(dst + (((uint32_t)j ^ sw) << 4));
+                const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  x[2 * i] += __uint_as_float(ww[i] << 16);
+                  x[2 * i + 1] += __uint_as_float(ww[i] & 0xFFFF0000u);
+                }
+              }
+            }
+          }
+          if (ragged) store_ragged<kOut4>(p, p.out, u.split * p.split_out + row * p.ld_out + col, col, x);
+          if constexpr (kOut4) {
+            *reinterpret_cast<float4*>(dst + (((2u * j) ^ sw) << 4)) = make_float4(x[0], x[1], x[2], x[3]);
+            *reinterpret_cast<float4*>(dst + (((2u * j + 1u) ^ sw) << 4)) = make_float4(x[4], x[5], x[6], x[7]);
+          } else {
+            *reinterpret_cast<uint4*>(dst + (((uint32_t)j ^ sw) << 4)) =
+                make_uint4(pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]), pack2_bf16(x[4], x[5]), pack2_bf16(x[6], x[7]));
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        group_all(group, true);
+        if (boss && col0 < p.whole_cols) {
+          store_box(&maps.out, stage_s + buf, col0, row0, u.split);
+          if (pre) store_box(&maps.pre, stage_s + kChunkBytes, col0, row0, 0);
+          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+        ++n_chunk;
+      }
+      if (kMode != kF32) ++it;
+    }
+    if (boss) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  }
+
+  // ---------------------------------------------------------------------------------------------- teardown
+  __syncwarp();
+  tc_fence_before();
+  cluster_sync();
+  if (warp == 2) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  }
+}
+
+// Persistent grid: one CTA pair per two SMs, as many as can be resident (kept per device and kernel).
+template <typename Kernel>
+int dense_grid(Kernel kernel, int* cached, int dev, cudaStream_t st, int* grid_out) {
+  int grid = dev >= 0 && dev < 64 ? cached[dev] : 0;
+  if (grid == 0) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return SWITCH_MOE_CUDA_ERROR;
+    const int sms = sm_count_or_default();
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3((unsigned)(sms & ~1));
+    lc.blockDim = dim3(kThreads);
+    lc.dynamicSmemBytes = kSmem;
+    lc.stream = st;
+    int clusters = 0;
+    if (cudaOccupancyMaxActiveClusters(&clusters, kernel, &lc) != cudaSuccess || clusters < 1) {
+      (void)cudaGetLastError();
+      clusters = sms / 2;
+    }
+    grid = 2 * (clusters < sms / 2 ? clusters : sms / 2);
+    if (grid < 2) return SWITCH_MOE_CUDA_ERROR;
+    if (dev >= 0 && dev < 64) cached[dev] = grid;
+  }
+  *grid_out = grid;
+  return SWITCH_MOE_OK;
+}
+
+template <bool kAMn, bool kBMn, int TN, int kMode>
+int launch_kernel(const DenseMaps& m, const DenseParams& p, cudaStream_t st) {
+  static int cached[64] = {0};
+  auto kernel = dense_gemm_kernel<kAMn, kBMn, TN, kMode>;
+  int dev = 0, grid = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return SWITCH_MOE_CUDA_ERROR;
+  const int rc = dense_grid(kernel, cached, dev, st, &grid);
+  if (rc != SWITCH_MOE_OK) return rc;
+  const long long units = (long long)p.m_tiles * p.n_tiles * p.splits;
+  if (2 * units < grid) grid = (int)(2 * units);
+  launch_k(kernel, dim3(grid), dim3(kThreads), kSmem, st, m, p);
+  return launch_status();
+}
+
+// Tile width: 128 columns where that makes the last round of the pairs so much fuller that it pays (a 128-wide tile
+// takes about 0.6 of a 256-wide one's time), or where there are no more columns.
+int tile_columns(long long rows, long long cols, long long splits) {
+  if (cols <= 128) return 128;
+  const long long pairs = kChipSms / 2, m = (rows + 255) / 256;
+  const long long wide = (m * ((cols + 255) / 256) * splits + pairs - 1) / pairs;
+  const long long slim = (m * ((cols + 127) / 128) * splits + pairs - 1) / pairs;
+  return 0.6 * (double)slim < (double)wide ? 128 : 256;
+}
+
+template <bool kAMn, bool kBMn, int kMode>
+int launch_kind(const DenseProduct& q, const DenseEpilogue& e, cudaStream_t st) {
+  const int TN = tile_columns(q.rows, q.cols, q.splits);
+  DenseParams p{};
+  p.rows = q.rows; p.cols = q.cols; p.k = q.k;
+  p.k_blocks = (int)(((long long)q.k + kBK - 1) / kBK);
+  const long long m_tiles = ((long long)q.rows + 255) / 256, n_tiles = ((long long)q.cols + TN - 1) / TN;
+  if (m_tiles * n_tiles * q.splits > 0x3fffffffll || n_tiles * kBand > 0x3fffffffll) return SWITCH_MOE_UNSUPPORTED_SHAPE;
+  p.m_tiles = (int)m_tiles; p.n_tiles = (int)n_tiles; p.splits = q.splits;
+  p.k_per_split = (p.k_blocks + q.splits - 1) / q.splits;
+  p.activation = e.activation; p.dropout_blocks = e.dropout_blocks; p.dropout = e.dropout; p.bias = e.bias;
+  p.has_residual = e.residual != nullptr; p.has_pre = e.pre != nullptr;
+  p.a = q.a.f32; p.a_si = q.a.si; p.a_sk = q.a.sk;
+  p.b = q.b.f32; p.b_si = q.b.si; p.b_sk = q.b.sk;
+  const int unit = kMode == kBf16 ? 8 : 4;
+  p.whole_cols = kMode == kPartial ? q.cols : q.cols / unit * unit;     // (part sums: rows padded to whole pieces)
+  p.out = q.out; p.pre = e.pre; p.ld_out = q.ld_out; p.split_out = (long long)q.rows * q.ld_out;
+  p.status = q.status; p.clear_status = q.clear_status ? 1 : 0;
+  DenseMaps m;
+  const int depth = q.f32 ? 3 : 1, elt = kMode == kBf16 ? 2 : 4;
+  int rc = kAMn ? make_map_rows(&m.a, q.a.p, 2, depth, q.k, q.rows, q.a.ld, 64) : make_map_rows(&m.a, q.a.p, 2, depth, q.rows, q.k, q.a.ld, 128);
+  if (rc == SWITCH_MOE_OK)
+    rc = kBMn ? make_map_rows(&m.b, q.b.p, 2, depth, q.k, q.cols, q.b.ld, 64) : make_map_rows(&m.b, q.b.p, 2, depth, q.cols, q.k, q.b.ld, TN / 2);
+  const long long stored = kMode == kPartial ? q.ld_out : p.whole_cols > 0 ? p.whole_cols : unit;
+  if (rc == SWITCH_MOE_OK) rc = make_map_rows(&m.out, q.out, elt, q.splits, q.rows, stored, q.ld_out, 128);
+  m.pre = m.out;
+  m.residual = m.out;
+  if (rc == SWITCH_MOE_OK && e.pre != nullptr) rc = make_map_rows(&m.pre, e.pre, elt, 1, q.rows, stored, q.ld_out, 128);
+  if (rc == SWITCH_MOE_OK && e.residual != nullptr) rc = make_map_rows(&m.residual, e.residual, elt, 1, q.rows, q.cols, q.ld_out, 128);
+  if (rc != SWITCH_MOE_OK) return rc;
+  return TN == 256 ? launch_kernel<kAMn, kBMn, 256, kMode>(m, p, st) : launch_kernel<kAMn, kBMn, 128, kMode>(m, p, st);
+}
+
+}  // namespace
+
+// Into how many parts the contraction is cut: where the output has too few tiles for the pairs, as in a weight gradient,
+// so that the last round of units is full; at least 16 blocks of 64 steps a part, whose sums are written and read once more.
+int dense_splits(long long rows, long long cols, long long k) {
+  const long long pairs = kChipSms / 2, tiles = ((rows + 255) / 256) * ((cols + 255) / 256), blocks = (k + kBK - 1) / kBK;
+  int best = 1;
+  double best_cost = 0;
+  for (int s = 1; s <= 16; ++s) {
+    const long long per = (blocks + s - 1) / s;
+    if (s > 1 && (per < 16 || (s - 1) * per >= blocks)) continue;
+    const long long rounds = (tiles * s + pairs - 1) / pairs;
+    // in blocks of a 256 x 256 tile, 0.3 us each: the products, and 256 KB a tile and part written and read at 6 TB/s by all pairs
+    const double cost = (double)rounds * (double)per + (s > 1 ? 8.0 + 0.3 * (double)(tiles * s) : 0.0);
+    if (best_cost == 0 || cost < best_cost) { best = s; best_cost = cost; }
+  }
+  return best;
+}
+
+int launch_dense(DenseKind kind, const DenseProduct& q, const DenseEpilogue& e, cudaStream_t st) {
+  const int mode = q.f32 ? kF32 : q.splits > 1 ? kPartial : kBf16;
+  if (kind == kDenseFwd) return mode == kF32 ? launch_kind<false, true, kF32>(q, e, st) : launch_kind<false, true, kBf16>(q, e, st);
+  if (kind == kDenseDx) return mode == kF32 ? launch_kind<false, false, kF32>(q, e, st) : launch_kind<false, false, kBf16>(q, e, st);
+  return mode == kF32 ? launch_kind<true, true, kF32>(q, e, st)
+                      : mode == kPartial ? launch_kind<true, true, kPartial>(q, e, st) : launch_kind<true, true, kBf16>(q, e, st);
+}
+
+}  // namespace swmoe

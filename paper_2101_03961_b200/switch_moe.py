@@ -32,6 +32,9 @@ EXPORTED_SYMBOLS = [
     "switch_moe_dispatch_plan_static", "switch_moe_step_host", "switch_moe_step_host_enqueue",
     "switch_moe_check_device_status", "switch_moe_launches_per_step", "switch_moe_stage_launches",
     "switch_moe_status_string",
+    "switch_moe_linear_workspace_bytes", "switch_moe_linear_fwd", "switch_moe_linear_bwd",
+    "switch_moe_linear_check_device_status", "switch_moe_dropout_fwd", "switch_moe_dropout_bwd",
+    "switch_moe_balance_workspace_bytes", "switch_moe_balance_fwd", "switch_moe_balance_bwd",
 ]
 
 
@@ -49,6 +52,37 @@ class SwitchMoeConfig(ctypes.Structure):
         ("router_jitter", ctypes.c_void_p),
         ("expert_keep", ctypes.c_void_p),
         ("expert_dropout", ctypes.c_float),
+    ]
+
+
+ACT_NONE, ACT_RELU, ACT_GELU = 0, 1, 2
+
+
+class LinearConfig(ctypes.Structure):
+    """Mirror of `switch_moe_linear_config`."""
+
+    _fields_ = [
+        ("M", ctypes.c_int32), ("K", ctypes.c_int32), ("N", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("activation", ctypes.c_int32), ("site", ctypes.c_int32), ("dropout", ctypes.c_float),
+        ("ldx", ctypes.c_int32), ("ldw", ctypes.c_int32), ("ldy", ctypes.c_int32), ("reserved", ctypes.c_int32 * 2),
+    ]
+
+
+class DropoutConfig(ctypes.Structure):
+    """Mirror of `switch_moe_dropout_config`."""
+
+    _fields_ = [
+        ("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("ld", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("site", ctypes.c_int32), ("rate", ctypes.c_float), ("reserved", ctypes.c_int32 * 2),
+    ]
+
+
+class BalanceConfig(ctypes.Structure):
+    """Mirror of `switch_moe_balance_config`."""
+
+    _fields_ = [
+        ("T", ctypes.c_int32), ("E", ctypes.c_int32), ("k", ctypes.c_int32), ("groups", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("ld", ctypes.c_int32), ("alpha", ctypes.c_float), ("reserved", ctypes.c_int32 * 2),
     ]
 
 
@@ -89,6 +123,16 @@ def load_library() -> ctypes.CDLL:
     lib.switch_moe_stage_launches.argtypes = [cp, i32p]
     lib.switch_moe_status_string.argtypes = [ctypes.c_int]
     lib.switch_moe_status_string.restype = ctypes.c_char_p
+    lp, dp, bp = ctypes.POINTER(LinearConfig), ctypes.POINTER(DropoutConfig), ctypes.POINTER(BalanceConfig)
+    lib.switch_moe_linear_workspace_bytes.argtypes = [lp, ctypes.c_int32, szp]
+    lib.switch_moe_linear_fwd.argtypes = [lp] + [vp] * 8 + [ctypes.c_size_t, vp]
+    lib.switch_moe_linear_bwd.argtypes = [lp] + [vp] * 6 + [ctypes.c_size_t] + [vp] * 4
+    lib.switch_moe_linear_check_device_status.argtypes = [lp, vp, i32p, vp]
+    lib.switch_moe_dropout_fwd.argtypes = [dp] + [vp] * 5
+    lib.switch_moe_dropout_bwd.argtypes = [dp] + [vp] * 4
+    lib.switch_moe_balance_workspace_bytes.argtypes = [bp, szp]
+    lib.switch_moe_balance_fwd.argtypes = [bp] + [vp] * 7 + [ctypes.c_size_t, vp]
+    lib.switch_moe_balance_bwd.argtypes = [bp] + [vp] * 4 + [ctypes.c_float, vp, vp]
     for name in EXPORTED_SYMBOLS:
         if name != "switch_moe_status_string":
             getattr(lib, name).restype = ctypes.c_int
@@ -278,3 +322,169 @@ def switch_moe_stage_launches(cfg) -> dict:
     out = (ctypes.c_int32 * (STAGE_EVENTS - 1))()
     _check(load_library().switch_moe_stage_launches(ctypes.byref(cfg), out), "switch_moe_stage_launches")
     return {name: int(out[i]) for i, name in enumerate(STAGE_NAMES) if name is not None}
+
+
+# ------------------------------------------------------------------ operators around the layer (switch_moe.h, second part)
+# These calls state rows and distances in their configs; a tensor that does not fit them is refused here, before its
+# pointer goes down.  (An int, taken as a device address, is the caller's word.)
+
+def make_linear_config(M, K, N, dtype=BF16, activation=ACT_NONE, dropout=0.0, site=0, ldx=0, ldw=0, ldy=0) -> LinearConfig:
+    """y = residual + dropout(activation(x W + bias)), x [M, K], W [K, N]; ld..: elements between rows, 0: dense."""
+    return LinearConfig(int(M), int(K), int(N), int(dtype), int(activation), int(site), float(dropout), int(ldx), int(ldw),
+                        int(ldy))
+
+
+def make_dropout_config(rows, cols, rate, dtype=BF16, site=0, ld=0) -> DropoutConfig:
+    return DropoutConfig(int(rows), int(cols), int(ld), int(dtype), int(site), float(rate))
+
+
+def make_balance_config(T, E, k=1, groups=1, alpha=0.01, dtype=F32, ld=0) -> BalanceConfig:
+    return BalanceConfig(int(T), int(E), int(k), int(groups), int(dtype), int(ld), float(alpha))
+
+
+_TORCH_TYPES = {BF16: torch.bfloat16, F32: torch.float32}
+
+
+def _refuse(where: str, name: str, why: str):
+    raise SwitchMoeError(INVALID_ARGUMENT, f"{where}: {name} {why}")
+
+
+def _matrix(where, name, t, dtype, rows, cols, ld):
+    """Pointer of a [rows, cols] tensor with `ld` elements between rows (0: cols), or of None."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype != _TORCH_TYPES.get(dtype):
+        _refuse(where, name, f"is {t.dtype}")
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        _refuse(where, name, f"is {tuple(t.shape)}, not {(rows, cols)}")
+    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) != (ld or cols)):
+        _refuse(where, name, f"has strides {t.stride()}, not {(ld or cols, 1)}")
+    return _on_device(where, name, t)
+
+
+def _vector(where, name, t, dtype, n):
+    """Pointer of a contiguous tensor of n elements, or of None."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
+        _refuse(where, name, f"is {t.dtype}")
+    if t.numel() != n or not t.is_contiguous():
+        _refuse(where, name, f"is {tuple(t.shape)} with strides {t.stride()}, not {n} contiguous elements")
+    return _on_device(where, name, t)
+
+
+def _on_device(where, name, t):
+    if not t.is_cuda:
+        _refuse(where, name, "is not on a GPU")
+    if t.device.index != (_device() if _device is not None else torch.cuda.current_device()):
+        _refuse(where, name, "is not on the current device")
+    return t.data_ptr()
+
+
+_RNG_TYPES = (torch.int64, torch.uint64)
+
+
+def _workspace_args(where, t):
+    if t is None:
+        return None, 0
+    if not t.is_contiguous():
+        _refuse(where, "workspace", "is not contiguous")
+    return _on_device(where, "workspace", t), t.numel() * t.element_size()
+
+
+def switch_moe_linear_workspace_bytes(cfg: LinearConfig, backward=False) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load_library().switch_moe_linear_workspace_bytes(ctypes.byref(cfg), int(backward), ctypes.byref(out)),
+           "switch_moe_linear_workspace_bytes")
+    return out.value
+
+
+def switch_moe_balance_workspace_bytes(cfg: BalanceConfig) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load_library().switch_moe_balance_workspace_bytes(ctypes.byref(cfg), ctypes.byref(out)),
+           "switch_moe_balance_workspace_bytes")
+    return out.value
+
+
+def _aligned_bytes(n: int, device) -> torch.Tensor:
+    raw = torch.empty(n + 1024, dtype=torch.uint8, device=device)
+    off = (-raw.data_ptr()) % 1024
+    return raw[off:off + n]
+
+
+def allocate_linear_workspace(cfg: LinearConfig, backward=False, device="cuda") -> torch.Tensor:
+    return _aligned_bytes(switch_moe_linear_workspace_bytes(cfg, backward), device)
+
+
+def allocate_balance_workspace(cfg: BalanceConfig, device="cuda") -> torch.Tensor:
+    return _aligned_bytes(switch_moe_balance_workspace_bytes(cfg), device)
+
+
+def switch_moe_linear_fwd(cfg, x, W, bias, residual, rng, y, pre, workspace, stream=None) -> None:
+    """x [M, K], W [K, N], bias float32 [N] or None, residual [M, N] or None, rng int64 [2] {key, offset} (None without
+    dropout); writes y [M, N] and, unless it is None, pre [M, N]."""
+    f, c = "switch_moe_linear_fwd", cfg
+    args = (_matrix(f, "x", x, c.dtype, c.M, c.K, c.ldx), _matrix(f, "W", W, c.dtype, c.K, c.N, c.ldw),
+            _vector(f, "bias", bias, torch.float32, c.N), _matrix(f, "residual", residual, c.dtype, c.M, c.N, c.ldy),
+            _vector(f, "rng", rng, _RNG_TYPES, 2), _matrix(f, "y", y, c.dtype, c.M, c.N, c.ldy),
+            _matrix(f, "pre", pre, c.dtype, c.M, c.N, c.ldy))
+    _check(load_library().switch_moe_linear_fwd(ctypes.byref(cfg), *args, *_workspace_args(f, workspace), _stream(stream)), f)
+
+
+def switch_moe_linear_bwd(cfg, dy, x, W, pre, rng, workspace, dx, dW, dbias, stream=None) -> None:
+    """Writes dx [M, K], dW [K, N], dbias float32 [N]; each may be None.  The residual's gradient is dy."""
+    f, c = "switch_moe_linear_bwd", cfg
+    ins = (_matrix(f, "dy", dy, c.dtype, c.M, c.N, c.ldy), _matrix(f, "x", x, c.dtype, c.M, c.K, c.ldx),
+           _matrix(f, "W", W, c.dtype, c.K, c.N, c.ldw), _matrix(f, "pre", pre, c.dtype, c.M, c.N, c.ldy),
+           _vector(f, "rng", rng, _RNG_TYPES, 2))
+    outs = (_matrix(f, "dx", dx, c.dtype, c.M, c.K, c.ldx), _matrix(f, "dW", dW, c.dtype, c.K, c.N, c.ldw),
+            _vector(f, "dbias", dbias, torch.float32, c.N))
+    _check(load_library().switch_moe_linear_bwd(ctypes.byref(cfg), *ins, *_workspace_args(f, workspace), *outs,
+                                                _stream(stream)), f)
+
+
+def switch_moe_linear_check_device_status(cfg, workspace, stream=None) -> list:
+    """Synchronises the stream; raises SwitchMoeError on a device-side timeout, returns the raw status words."""
+    info = (ctypes.c_int32 * 16)()
+    rc = load_library().switch_moe_linear_check_device_status(ctypes.byref(cfg), _ptr(workspace), info, _stream(stream))
+    if rc != OK:
+        raise SwitchMoeError(rc, f"switch_moe_linear_check_device_status info={list(info)}")
+    return list(info)
+
+
+def switch_moe_dropout_fwd(cfg, x, residual, rng, y, stream=None) -> None:
+    """y = residual + dropout(x); residual may be None, y may be x or residual."""
+    f, c = "switch_moe_dropout_fwd", cfg
+    m = lambda name, t: _matrix(f, name, t, c.dtype, c.rows, c.cols, c.ld)
+    _check(load_library().switch_moe_dropout_fwd(ctypes.byref(cfg), m("x", x), m("residual", residual),
+                                                 _vector(f, "rng", rng, _RNG_TYPES, 2), m("y", y), _stream(stream)), f)
+
+
+def switch_moe_dropout_bwd(cfg, dy, rng, dx, stream=None) -> None:
+    """dx = dropout(dy) with the mask of the forward call; dx may be dy."""
+    f, c = "switch_moe_dropout_bwd", cfg
+    m = lambda name, t: _matrix(f, name, t, c.dtype, c.rows, c.cols, c.ld)
+    _check(load_library().switch_moe_dropout_bwd(ctypes.byref(cfg), m("dy", dy), _vector(f, "rng", rng, _RNG_TYPES, 2),
+                                                 m("dx", dx), _stream(stream)), f)
+
+
+def switch_moe_balance_fwd(cfg, logits, expert_index, token_mask, loss, counts, tokens, workspace, stream=None) -> None:
+    """logits [T, E]; expert_index int32 [T, k] or None (the k largest logits); token_mask uint8 or bool [T] or None; writes
+    loss float32 [1], counts int32 [groups, E], tokens int32 [groups]."""
+    f, c = "switch_moe_balance_fwd", cfg
+    G = c.groups or 1
+    args = (_matrix(f, "logits", logits, c.dtype, c.T, c.E, c.ld), _vector(f, "expert_index", expert_index, torch.int32, c.T * c.k),
+            _vector(f, "token_mask", token_mask, (torch.uint8, torch.bool), c.T), _vector(f, "loss", loss, torch.float32, 1),
+            _vector(f, "counts", counts, torch.int32, G * c.E), _vector(f, "tokens", tokens, torch.int32, G))
+    _check(load_library().switch_moe_balance_fwd(ctypes.byref(cfg), *args, *_workspace_args(f, workspace), _stream(stream)), f)
+
+
+def switch_moe_balance_bwd(cfg, logits, token_mask, counts, tokens, d_loss, dlogits, stream=None) -> None:
+    """dlogits [T, E] from the counts and tokens of the forward call; dlogits may be logits."""
+    f, c = "switch_moe_balance_bwd", cfg
+    G = c.groups or 1
+    _check(load_library().switch_moe_balance_bwd(
+        ctypes.byref(cfg), _matrix(f, "logits", logits, c.dtype, c.T, c.E, c.ld),
+        _vector(f, "token_mask", token_mask, (torch.uint8, torch.bool), c.T), _vector(f, "counts", counts, torch.int32, G * c.E),
+        _vector(f, "tokens", tokens, torch.int32, G), float(d_loss),
+        _matrix(f, "dlogits", dlogits, c.dtype, c.T, c.E, c.ld), _stream(stream)), f)
