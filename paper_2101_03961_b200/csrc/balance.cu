@@ -45,8 +45,8 @@ int resolve(const switch_moe_balance_config* cfg, BalanceShape* s) {
   s->T = c.T; s->E = c.E; s->k = c.k; s->G = G; s->Tg = c.T / G;
   s->ld = c.ld > 0 ? c.ld : c.E;
   s->alpha = c.alpha; s->f32 = c.dtype == SWITCH_MOE_F32;
-  // about two blocks per SM over all groups, each with 8 rows a warp or more
-  long long want = ((long long)2 * kChipSms + G - 1) / G, most = (s->Tg + 8 * kWarps - 1) / (8 * kWarps);
+  // about four blocks per SM over all groups, each with 8 rows a warp or more
+  long long want = ((long long)4 * kChipSms + G - 1) / G, most = (s->Tg + 8 * kWarps - 1) / (8 * kWarps);
   s->blocks = (int)(want < most ? want : most);
   if (s->blocks < 1) s->blocks = 1;
   return SWITCH_MOE_OK;
@@ -132,24 +132,29 @@ struct Row {
       }
     }
   }
-  // In place: x becomes the softmax; returns whether the row counts (some logit is not -infinity).  A NaN anywhere, or
-  // +infinity, makes the row's probabilities NaN, as in the definition.
-  __device__ __forceinline__ bool softmax(int L, float* max_out) {
+  // p = the softmax; returns whether the row counts (some logit is not -infinity).  A NaN anywhere, or +infinity, makes the
+  // row's probabilities NaN, as in the definition: through the sum, which only a row without a finite maximum does not show.
+  __device__ __forceinline__ bool softmax(int L, float* p, float* max_out) const {
     float m = -INFINITY;
-    int nan = 0;
 #pragma unroll
-    for (int i = 0; i < V * NV; ++i) { m = fmaxf(m, x[i]); nan |= isnan(x[i]) ? 1 : 0; }
+    for (int i = 0; i < V * NV; ++i) m = fmaxf(m, x[i]);
     m = lane_max(m, L);
-    nan = lane_or(nan, L);
     *max_out = m;
-    const bool counts = m != -INFINITY || nan != 0;
+    bool counts = true;
+    if (__any_sync(0xffffffffu, m == -INFINITY)) {
+      int nan = 0;
+#pragma unroll
+      for (int i = 0; i < V * NV; ++i) nan |= isnan(x[i]) ? 1 : 0;
+      nan = lane_or(nan, L);
+      counts = m != -INFINITY || nan != 0;
+    }
     float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < V * NV; ++i) { x[i] = expf(x[i] - m); s += x[i]; }
+    for (int i = 0; i < V * NV; ++i) { p[i] = expf(x[i] - m); s += p[i]; }
     s = lane_sum(s, L);
     const float r = 1.f / s;
 #pragma unroll
-    for (int i = 0; i < V * NV; ++i) x[i] *= r;
+    for (int i = 0; i < V * NV; ++i) p[i] *= r;
     return counts;
   }
 };
@@ -185,15 +190,14 @@ balance_rows_kernel(const ET* logits, const int* index, const uint8_t* mask, Bal
   Row<ET, V, NV> next;
   bool next_valid = first < s.Tg && fetch(first, next);
   for (int t = first; t < s.Tg; t += stride) {
-    Row<ET, V, NV> r = next, raw;
+    const Row<ET, V, NV> raw = next;
     const bool valid = next_valid;
     if (t + stride < s.Tg) next_valid = fetch(t + stride, next);
-    raw = r;
-    float m;
-    const bool used = r.softmax(L, &m) && valid;
+    float m, p[V * NV];
+    const bool used = raw.softmax(L, p, &m) && valid;
     if (used) {
 #pragma unroll
-      for (int i = 0; i < V * NV; ++i) acc[i] += (l + (i / V) * L) * V + i % V < s.E ? r.x[i] : 0.f;
+      for (int i = 0; i < V * NV; ++i) acc[i] += p[i];        // (sums beyond E are never stored)
       n += l == 0;
     }
     if (index != nullptr) {
@@ -336,11 +340,11 @@ balance_bwd_kernel(const ET* logits, const uint8_t* mask, const int* counts, con
     const bool valid = at < s.Tg && (mask == nullptr || mask[row0 + at] != 0);
     Row<ET, V, NV> r;
     r.load(logits + (row0 + (valid ? at : 0)) * s.ld, valid, l, L, s.E);
-    float m;
-    const bool used = r.softmax(L, &m) && valid;
+    float m, p[V * NV];
+    const bool used = r.softmax(L, p, &m) && valid;
     float dot = 0.f;
 #pragma unroll
-    for (int i = 0; i < V * NV; ++i) dot += r.x[i] * grad[i];
+    for (int i = 0; i < V * NV; ++i) dot += p[i] * grad[i];
     dot = lane_sum(dot, L);
     if (at < s.Tg) {
       ET* out = dlogits + (row0 + at) * s.ld;
@@ -349,7 +353,7 @@ balance_bwd_kernel(const ET* logits, const uint8_t* mask, const int* counts, con
         const int p0 = (l + j * L) * V;
         float o[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) o[i] = used ? r.x[j * V + i] * (grad[j * V + i] - dot) : 0.f;
+        for (int i = 0; i < V; ++i) o[i] = used ? p[j * V + i] * (grad[j * V + i] - dot) : 0.f;
         if (p0 < s.E) Piece<ET, V>::store(out + p0, o);
       }
     }
@@ -362,8 +366,10 @@ int with_layout(const BalanceShape& s, bool vector, F&& f) {
   constexpr int W = 16 / (int)sizeof(ET);
   const int V = vector ? W : 1;
   const int pieces = (s.E + V - 1) / V;
+  // Few lanes a row, 16 elements each, so that the rows of a warp share the steps of its reductions; but four lanes at
+  // least (64 consecutive bytes), and with single elements as many as there are.
   int L = 1;
-  while (L < 32 && L < pieces) L *= 2;
+  while (L < 32 && L < pieces && (V == 1 || L < 4 || pieces * V > 16 * L)) L *= 2;
   const int nv = (pieces + L - 1) / L;
   using std::integral_constant;
 #define SWMOE_NV(vv, n) \

@@ -9,7 +9,8 @@ namespace swmoe {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kColsPerBlock = 256, kRowLanes = 8;    // 32 threads x 8 columns, 8 rows at a time
+constexpr int kColsPerBlock = 256, kRowLanes = 8;    // 32 threads x 8 columns, 8 rows side by side,
+constexpr int kRowsAhead = 4, kDzStep = kRowLanes * kRowsAhead;   // four of them per thread in flight
 
 struct LinearShape {
   int M, K, N, act, q, site;
@@ -43,14 +44,11 @@ int resolve(const switch_moe_linear_config* cfg, LinearShape* s) {
   s->ldn = ((long long)c.N + 7) / 8 * 8;
   s->ldk = ((long long)c.K + 7) / 8 * 8;
   if ((long long)c.M * (s->ldn / 8) >= 1ll << 48) return SWITCH_MOE_UNSUPPORTED_SHAPE;
-  // about eight blocks per SM, each with at least 32 rows
+  // chunks of 64 rows: many short blocks keep the SMs evenly busy; longer ones where that would be more than 1024 chunks
   const long long col_blocks = ((long long)c.N + kColsPerBlock - 1) / kColsPerBlock;
-  long long chunks = (8ll * kChipSms + col_blocks - 1) / col_blocks, most = ((long long)c.M + 31) / 32;
-  if (chunks > most) chunks = most;
-  if (chunks < 1) chunks = 1;
-  long long rows = ((long long)c.M + chunks - 1) / chunks;
-  rows = (rows + kRowLanes - 1) / kRowLanes * kRowLanes;
-  if (rows < kRowLanes) rows = kRowLanes;
+  long long rows = ((long long)c.M + 1023) / 1024;
+  rows = (rows + kDzStep - 1) / kDzStep * kDzStep;
+  if (rows < 2 * kDzStep) rows = 2 * kDzStep;
   s->chunk_rows = (int)rows;
   s->chunks = (int)(((long long)c.M + rows - 1) / rows);
   if (s->chunks > 65535 || col_blocks > 0x7fffffffll) return SWITCH_MOE_UNSUPPORTED_SHAPE;
@@ -75,17 +73,6 @@ void make_plan(const LinearShape& s, LinearPlan* p) {
 }
 
 // Eight consecutive elements of a row, the first `n` of them inside; 16-byte aligned.
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, int n, float* f) {
-  if (n >= 8) {
-    const uint4 v = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = i < n ? __bfloat162float(p[i]) : 0.f;
-  }
-}
 __device__ __forceinline__ void load8(const float* p, int n, float* f) {
   if (n >= 8) {
 #pragma unroll
@@ -98,6 +85,35 @@ __device__ __forceinline__ void load8(const float* p, int n, float* f) {
     for (int i = 0; i < 8; ++i) f[i] = i < n ? p[i] : 0.f;
   }
 }
+// The same in flight: loaded now, converted when it is needed.
+template <typename ET> struct Raw8;
+template <> struct Raw8<__nv_bfloat16> {
+  uint4 v;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p, int n) {
+    if (n >= 8) {
+      v = *reinterpret_cast<const uint4*>(p);
+    } else {
+      const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = (2 * i < n ? q[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)q[2 * i + 1] << 16 : 0u);
+      v = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+  __device__ __forceinline__ void get(float* f) const {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+  }
+};
+template <> struct Raw8<float> {
+  float f8[8];
+  __device__ __forceinline__ void load(const float* p, int n) { load8(p, n, f8); }
+  __device__ __forceinline__ void get(float* f) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = f8[i];
+  }
+};
 __device__ __forceinline__ void store8(__nv_bfloat16* p, int n, const float* f) {
   if (n >= 8) {
     uint4 v;
@@ -135,15 +151,16 @@ __device__ __forceinline__ void store_parts8(__nv_bfloat16* p, long long plane, 
   store8(p + 2 * plane, 8, l);
 }
 
-// dz and the bias gradient.  A block takes 256 columns of a chunk of rows: 32 threads x 8 columns, 8 rows at a time; its
-// column sums go to `part`, from where they are added up in chunk order.
+// dz and the bias gradient.  A block takes 256 columns of a chunk of rows: 32 threads x 8 columns, 8 rows side by side; a
+// thread asks for four of its rows before it works on the first.  Column sums go to `part`, from where they are added up in
+// chunk order.  Bound by reading dy and pre and writing dz once.
 struct DzArgs {
   int M, N, act, chunk_rows, per_row;
   long long ldy, ldn;
   DropoutParams dropout;
 };
-template <typename ET>
-__global__ void __launch_bounds__(kThreads)
+template <typename ET, int kAct>
+__global__ void __launch_bounds__(kThreads, 3)
 linear_dz_kernel(const ET* __restrict__ dy, const ET* __restrict__ pre, DzArgs a, ET* dz, __nv_bfloat16* parts, float* part, int* status) {
   pdl_launch_dependents();
   pdl_wait();
@@ -158,30 +175,48 @@ linear_dz_kernel(const ET* __restrict__ dy, const ET* __restrict__ pre, DzArgs a
   for (int i = 0; i < 8; ++i) acc[i] = 0.f;
   const long long row_end = min((long long)a.M, (long long)(blockIdx.y + 1) * a.chunk_rows);
   if (n > 0) {
-#pragma unroll 2
-    for (long long row = (long long)blockIdx.y * a.chunk_rows + ry; row < row_end; row += kRowLanes) {
-      float g[8], z[8];
-      load8(dy + row * a.ldy + col, n, g);
-      if (a.act != SWITCH_MOE_ACT_NONE) load8(pre + row * a.ldy + col, n, z);
-      if (a.dropout.rng != nullptr) {
-        const uint4 bits = dropout_bits(a.dropout, rng, (unsigned long long)row * (unsigned)a.per_row + (unsigned)(col >> 3));
+#pragma unroll 1
+    for (long long row0 = (long long)blockIdx.y * a.chunk_rows + ry; row0 < row_end; row0 += kDzStep) {
+      Raw8<ET> graw[kRowsAhead], zraw[kRowsAhead];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float f = dropout_factor(a.dropout, bits, i);
-          g[i] = f != 0.f ? g[i] * f : 0.f;
+      for (int k = 0; k < kRowsAhead; ++k) {
+        const long long row = row0 + k * kRowLanes;
+        if (row < row_end) {
+          graw[k].load(dy + row * a.ldy + col, n);
+          if (kAct != SWITCH_MOE_ACT_NONE) zraw[k].load(pre + row * a.ldy + col, n);
         }
       }
-      if (a.act == SWITCH_MOE_ACT_RELU) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) g[i] = z[i] > 0.f ? g[i] : 0.f;
-      } else if (a.act == SWITCH_MOE_ACT_GELU) {
+      for (int k = 0; k < kRowsAhead; ++k) {
+        const long long row = row0 + k * kRowLanes;
+        if (row >= row_end) break;
+        float g[8], z[8];
+        graw[k].get(g);
+        if (a.dropout.rng != nullptr) {
+          const uint4 bits = dropout_bits(a.dropout, rng, (unsigned long long)row * (unsigned)a.per_row + (unsigned)(col >> 3));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) g[i] *= activation_derivative(SWITCH_MOE_ACT_GELU, z[i]);
+          for (int i = 0; i < 8; ++i) {
+            const float f = dropout_factor(a.dropout, bits, i);
+            g[i] = f != 0.f ? g[i] * f : 0.f;
+          }
+        }
+        if (kAct != SWITCH_MOE_ACT_NONE) zraw[k].get(z);
+        if (kAct == SWITCH_MOE_ACT_RELU) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) g[i] = z[i] > 0.f ? g[i] : 0.f;
+        } else if (kAct == SWITCH_MOE_ACT_GELU) {
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) {
+            const float2 d = gelu_grad_pair(z[i], z[i + 1]);
+            g[i] *= d.x;
+            g[i + 1] *= d.y;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] += g[i];
+        if (dz != nullptr) store8(dz + row * a.ldn + col, 8, g);        // (the workspace's rows are multiples of 8)
+        if (parts != nullptr) store_parts8(parts + row * a.ldn + col, (long long)a.M * a.ldn, g);
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) acc[i] += g[i];
-      if (dz != nullptr) store8(dz + row * a.ldn + col, 8, g);          // (the workspace's rows are multiples of 8)
-      if (parts != nullptr) store_parts8(parts + row * a.ldn + col, (long long)a.M * a.ldn, g);
     }
   }
   if (part == nullptr) return;
@@ -195,25 +230,26 @@ linear_dz_kernel(const ET* __restrict__ dy, const ET* __restrict__ pre, DzArgs a
   if (c < a.N) part[(long long)blockIdx.y * a.ldn + c] = s;
 }
 
-// db[c] = sum over chunks: 32 columns per block, 8 chunks at a time.
-__global__ void __launch_bounds__(kThreads)
+// db[c] = sum over chunks: 32 columns per block, 32 chunks at a time.
+__global__ void __launch_bounds__(1024)
 linear_db_kernel(const float* __restrict__ part, int chunks, int N, long long ldn, float* db) {
   pdl_launch_dependents();
   pdl_wait();
-  __shared__ float sums[8][32];
+  __shared__ float sums[32][33];
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const long long c = (long long)blockIdx.x * 32 + lane;
   float s = 0.f;
-  if (c < N)
-    for (int i = w; i < chunks; i += 8) s += part[(long long)i * ldn + c];
+  if (c < N) {
+#pragma unroll 4
+    for (int i = w; i < chunks; i += 32) s += part[(long long)i * ldn + c];
+  }
   sums[w][lane] = s;
   __syncthreads();
-  if (w == 0 && c < N) {
-    s = 0.f;
+  s = sums[lane][w];                                  // column w, the 32 lanes hold its parts
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += sums[i][lane];
-    db[c] = s;
-  }
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  const long long out = (long long)blockIdx.x * 32 + w;
+  if (lane == 0 && out < N) db[out] = s;
 }
 
 // The parts of a float32 matrix, eight elements of a row per thread.
@@ -269,8 +305,15 @@ template <typename ET>
 int launch_dz(const LinearShape& s, const void* dy, const void* pre, const uint64_t* rng, void* dz, __nv_bfloat16* parts,
               float* part, int* status, cudaStream_t st) {
   DzArgs a{s.M, s.N, s.act, s.chunk_rows, (int)(s.ldn / 8), s.ldy, s.ldn, dropout_params(rng, s.q, s.site)};
-  launch_k(linear_dz_kernel<ET>, dim3((unsigned)((s.N + kColsPerBlock - 1) / kColsPerBlock), s.chunks), dim3(kThreads), 0, st,
-           static_cast<const ET*>(dy), static_cast<const ET*>(pre), a, static_cast<ET*>(dz), parts, part, status);
+  const dim3 grid((unsigned)((s.N + kColsPerBlock - 1) / kColsPerBlock), s.chunks);
+  const ET* g = static_cast<const ET*>(dy);
+  const ET* z = static_cast<const ET*>(pre);
+  if (s.act == SWITCH_MOE_ACT_RELU)
+    launch_k(linear_dz_kernel<ET, SWITCH_MOE_ACT_RELU>, grid, dim3(kThreads), 0, st, g, z, a, static_cast<ET*>(dz), parts, part, status);
+  else if (s.act == SWITCH_MOE_ACT_GELU)
+    launch_k(linear_dz_kernel<ET, SWITCH_MOE_ACT_GELU>, grid, dim3(kThreads), 0, st, g, z, a, static_cast<ET*>(dz), parts, part, status);
+  else
+    launch_k(linear_dz_kernel<ET, SWITCH_MOE_ACT_NONE>, grid, dim3(kThreads), 0, st, g, z, a, static_cast<ET*>(dz), parts, part, status);
   return launch_status();
 }
 
@@ -367,7 +410,7 @@ extern "C" int switch_moe_linear_bwd(const switch_moe_linear_config* cfg, const 
     cleared = true;
   }
   if (dbias != nullptr) {
-    launch_k(linear_db_kernel, dim3((unsigned)((s.N + 31) / 32)), dim3(kThreads), 0, st, static_cast<const float*>(db_part),
+    launch_k(linear_db_kernel, dim3((unsigned)((s.N + 31) / 32)), dim3(1024), 0, st, static_cast<const float*>(db_part),
              s.chunks, s.N, s.ldn, dbias);
     SWMOE_TRY(launch_status());
   }

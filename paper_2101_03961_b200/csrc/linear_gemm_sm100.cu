@@ -51,7 +51,7 @@ struct DenseParams {
   const float* a; long long a_si, a_sk;
   const float* b; long long b_si, b_sk;
   int whole_cols;                                    // columns in whole 16-byte pieces: a TMA store clips at these, the rest
-  void* out; void* pre; long long ld_out, split_out; // of a row is written by the threads themselves
+  void* out; void* pre; const void* residual; long long ld_out, split_out; // of a row is written by the threads themselves
   int* status;
   int clear_status;
 };
@@ -302,15 +302,42 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
     if (kFwd) rng = dropout_state(p.dropout);
     uint32_t it = 0, n_chunk = 0, res_phase = 0;             // res_phase: a bit per buffer
     bool ok = true;
-    constexpr int kSums = kMode == kF32 ? TN / 2 : 1;
+    // The result of eight columns: bias, activation, dropout.  `saved` is called with z.
+    auto finish = [&](float* x, const float* bias8, long long row, int col, auto&& saved) {
+      if constexpr (kFwd) {
+        if (p.bias != nullptr) {
+          const float4 b0 = *reinterpret_cast<const float4*>(bias8), b1 = *reinterpret_cast<const float4*>(bias8 + 4);
+          x[0] += b0.x; x[1] += b0.y; x[2] += b0.z; x[3] += b0.w;
+          x[4] += b1.x; x[5] += b1.y; x[6] += b1.z; x[7] += b1.w;
+        }
+        if (pre) saved(x);
+        if (p.activation == SWITCH_MOE_ACT_RELU) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = x[i] < 0.f ? 0.f : x[i];          // (NaN stays)
+        } else if (p.activation == SWITCH_MOE_ACT_GELU) {
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) gelu_pair(x + i, x + i + 1);
+        }
+        if (p.dropout.rng != nullptr) {
+          const uint4 bits = dropout_bits(p.dropout, rng, (unsigned long long)row * (unsigned)p.dropout_blocks + (unsigned)(col >> 3));
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float f = dropout_factor(p.dropout, bits, i);
+            x[i] = f != 0.f ? x[i] * f : 0.f;
+          }
+        }
+      }
+    };
     for (int id = pair; id < n_units && ok; id += n_pairs) {
       const Unit u = decode(p, id, TN);
       const int row0 = u.m0 + 128 * (int)rank;
       const long long row = row0 + r;
-      float sum[kSums];
-      uint32_t taddr = 0;
       if constexpr (kMode == kF32) {
-        // a group holds one half of the tile's columns, a chunk of 32 after the other
+        // A group holds one half of the tile's columns.  Blocks of the contraction are added up in registers; the sums then
+        // go through shared memory two chunks of 32 columns at a time, so that what follows is a loop and not TN / 16
+        // copies of its code.
+        constexpr int kSums = TN / 2;
+        float sum[kSums];
 #pragma unroll
         for (int i = 0; i < kSums; ++i) sum[i] = 0.f;
         for (int kb = u.kb0; kb < u.kb1; ++kb, ++it) {
@@ -318,7 +345,7 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
           ok = mbar_wait_warp<true>(afull0 + 8u * side, (it >> 1) & 1u, abort_flag, p.status, 44);
           if (!ok) break;
           tc_fence_after();
-          taddr = tmem + ((uint32_t)(lg * 32) << 16) + side * TN + group * (TN / 2);
+          const uint32_t taddr = tmem + ((uint32_t)(lg * 32) << 16) + side * TN + group * (TN / 2);
 #pragma unroll
           for (int c = 0; c < TN / 64; ++c) {
             uint32_t v[32];
@@ -333,70 +360,34 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
             for (int i = 0; i < 32; ++i) sum[32 * c + i] += __uint_as_float(v[i]);
           }
         }
-      } else {
-        const uint32_t side = it & 1u;
-        ok = mbar_wait_warp(afull0 + 8u * side, (it >> 1) & 1u, abort_flag, p.status, 44);
-        taddr = tmem + ((uint32_t)(lg * 32) << 16) + side * TN;
-      }
-      if (!group_all(group, ok)) { ok = false; break; }
-      if (kMode != kF32) tc_fence_after();
-      constexpr int kMine = TN / kChunk / 2;                 // chunks of a group
-#pragma unroll
-      for (int c = 0; c < kMine; ++c) {
-        const int chunk = kMode == kF32 ? group * kMine + c : 2 * c + group;
-        const int col0 = u.n0 + chunk * kChunk;
-        const bool inside = col0 < p.cols && row0 < p.rows;  // the same in the whole group
-        uint32_t v[kMode == kBf16 ? 64 : 32];
-        if constexpr (kMode != kF32) {
-          tc_ld32(taddr + (uint32_t)(chunk * kChunk), v);
-          if constexpr (kMode == kBf16) tc_ld32(taddr + (uint32_t)(chunk * kChunk + 32), v + 32);
-        }
-        const uint32_t buf = pre ? 0u : (n_chunk & 1u) * kChunkBytes;
-        if (inside) {
-          if (boss) {                                        // the buffers of this chunk have been read by their last stores
-            if (pre) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-            else asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-            if (residual) {
-              const uint32_t rb = res0 + 16u * group + (buf ? 8u : 0u);
-              mbar_arrive_expect_tx(rb, kChunkBytes);
-              tma_load_3d(stage_s + buf, &maps.residual, rb, col0, row0, 0);
-            }
-          }
-          if (kFwd && p.bias != nullptr && t < kChunk) bias_g[t] = col0 + t < p.cols ? p.bias[col0 + t] : 0.f;
-          if (residual) {
-            const uint32_t bit = buf ? 2u : 1u;
-            ok = mbar_wait_warp<kProgress>(res0 + 16u * group + (buf ? 8u : 0u), (res_phase & bit) ? 1u : 0u, abort_flag, p.status, 45);
-            res_phase ^= bit;
-          }
-        }
-        __syncwarp();
-        if constexpr (kMode != kF32) {
-          wait_ld(v);
-          if constexpr (kMode == kBf16) wait_ld(v + 32);
-          if (c == kMine - 1) {                              // the accumulator has been read out
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) arrive_at(aempty0 + 8u * (it & 1u), 0);
-          }
-        }
-        if (!inside) continue;
         if (!group_all(group, ok)) { ok = false; break; }
-        uint8_t* dst = stage_g + buf + row_off;
+#pragma unroll 1
+        for (int half = 0; half < TN / 128; ++half) {
+          if (boss) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+          group_all(group, true);
+          auto dump = [&](const float* s) {
 #pragma unroll
-        for (int j = 0; j < kChunk / 8; ++j) {
-          float x[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            if constexpr (kMode == kF32) x[i] = sum[32 * c + 8 * j + i] * kPartDown;
-            else x[i] = __uint_as_float(v[8 * j + i]);
-          }
-          const int col = col0 + 8 * j;
-          const bool ragged = col + 8 > p.whole_cols && col < p.cols && row < p.rows;
-          if constexpr (kMode == kF32) {
+            for (int i = 0; i < 16; ++i)
+              *reinterpret_cast<float4*>(stage_g + (i >> 3) * kChunkBytes + row_off + (((uint32_t)(i & 7) ^ sw) << 4)) =
+                  make_float4(s[4 * i], s[4 * i + 1], s[4 * i + 2], s[4 * i + 3]);
+          };
+          if (TN == 128 || half == 0) dump(sum);
+          else dump(sum + (TN == 256 ? 64 : 0));
+#pragma unroll 1
+          for (int j = 0; j < 8; ++j) {
+            const int col = u.n0 + group * (TN / 2) + 64 * half + 8 * j;
+            if (col >= p.cols || row >= p.rows) break;
+            float4* at0 = reinterpret_cast<float4*>(stage_g + (j >> 2) * kChunkBytes + row_off + (((uint32_t)(2 * (j & 3)) ^ sw) << 4));
+            float4* at1 = reinterpret_cast<float4*>(stage_g + (j >> 2) * kChunkBytes + row_off + (((uint32_t)(2 * (j & 3) + 1) ^ sw) << 4));
+            const float4 lo = *at0, hi = *at1;
+            float x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
             bool finite = true;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) finite = finite && isfinite(x[i]);
-            if (!finite && row < p.rows) {
+            for (int i = 0; i < 8; ++i) {
+              x[i] *= kPartDown;
+              finite = finite && isfinite(x[i]);
+            }
+            if (!finite) {
 #pragma unroll 1
               for (int i = 0; i < 8; ++i) {
                 if (col + i >= p.cols) break;
@@ -412,75 +403,140 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
                   store_at(bars + 204u, cta, (uint32_t)clock64());
               }
             }
-          }
-          if constexpr (kFwd) {
-            if (p.bias != nullptr) {
+            float b8[8];
+            if (kFwd && p.bias != nullptr) {
 #pragma unroll
-              for (int i = 0; i < 8; ++i) x[i] += bias_g[8 * j + i];
+              for (int i = 0; i < 8; ++i) b8[i] = col + i < p.cols ? p.bias[col + i] : 0.f;
             }
-            if (pre) {
-              if (ragged) store_ragged<kOut4>(p, p.pre, row * p.ld_out + col, col, x);
-              uint8_t* pd = stage_g + kChunkBytes + row_off;
-              if constexpr (kOut4) {
-                *reinterpret_cast<float4*>(pd + (((2u * j) ^ sw) << 4)) = make_float4(x[0], x[1], x[2], x[3]);
-                *reinterpret_cast<float4*>(pd + (((2u * j + 1u) ^ sw) << 4)) = make_float4(x[4], x[5], x[6], x[7]);
+            const long long at = row * p.ld_out + col;
+            const bool whole = col + 8 <= p.whole_cols;
+            finish(x, b8, row, col, [&](const float* z) {
+              float* o = static_cast<float*>(p.pre) + at;
+              if (whole) {
+                *reinterpret_cast<float4*>(o) = make_float4(z[0], z[1], z[2], z[3]);
+                *reinterpret_cast<float4*>(o + 4) = make_float4(z[4], z[5], z[6], z[7]);
               } else {
-                *reinterpret_cast<uint4*>(pd + (((uint32_t)j ^ sw) << 4)) =
-                    make_uint4(pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]), pack2_bf16(x[4], x[5]), pack2_bf16(x[6], x[7]));
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                  if (col + i < p.cols) o[i] = z[i];
               }
-            }
-            if (p.activation == SWITCH_MOE_ACT_RELU) {
-#pragma unroll
-              for (int i = 0; i < 8; ++i) x[i] = x[i] < 0.f ? 0.f : x[i];      // (NaN stays)
-            } else if (p.activation == SWITCH_MOE_ACT_GELU) {
-#pragma unroll
-              for (int i = 0; i < 8; ++i) x[i] = gelu_exact(x[i]);
-            }
-            if (p.dropout.rng != nullptr) {
-              const uint4 bits = dropout_bits(p.dropout, rng, (unsigned long long)row * (unsigned)p.dropout_blocks + (unsigned)(col >> 3));
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const float f = dropout_factor(p.dropout, bits, i);
-                x[i] = f != 0.f ? x[i] * f : 0.f;
-              }
-            }
+            });
             if (residual) {
-              if constexpr (kOut4) {
+              const float* rs = static_cast<const float*>(p.residual) + at;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                  const float4 f = *reinterpret_cast<const float4*>(dst + (((2u * j + h) ^ sw) << 4));
-                  x[4 * h] += f.x; x[4 * h + 1] += f.y; x[4 * h + 2] += f.z; x[4 * h + 3] += f.w;
-                }
-              } else {
-                const uint4 w = *reinterpret_cast<const uint4*>(dst + (((uint32_t)j ^ sw) << 4));
-                const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+              for (int i = 0; i < 8; ++i)
+                if (col + i < p.cols) x[i] += rs[i];
+            }
+            if (!whole) store_ragged<true>(p, p.out, u.split * p.split_out + at, col, x);
+            *at0 = make_float4(x[0], x[1], x[2], x[3]);
+            *at1 = make_float4(x[4], x[5], x[6], x[7]);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          group_all(group, true);
+          if (boss) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  x[2 * i] += __uint_as_float(ww[i] << 16);
-                  x[2 * i + 1] += __uint_as_float(ww[i] & 0xFFFF0000u);
-                }
+            for (int c = 0; c < 2; ++c) {
+              const int col0 = u.n0 + group * (TN / 2) + 64 * half + 32 * c;
+              if (col0 < p.whole_cols && row0 < p.rows) store_box(&maps.out, stage_s + c * kChunkBytes, col0, row0, u.split);
+            }
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          }
+        }
+      } else {
+        const uint32_t side = it & 1u;
+        ok = mbar_wait_warp(afull0 + 8u * side, (it >> 1) & 1u, abort_flag, p.status, 44);
+        if (!group_all(group, ok)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t taddr = tmem + ((uint32_t)(lg * 32) << 16) + side * TN;
+        // A group takes every second chunk, 32 columns of it at a time; the next 32 are on their way from tensor memory
+        // meanwhile.  (Loops, not copies: with the epilogue's code once per column block it streams through the
+        // instruction caches.)
+        constexpr int kParts32 = kChunk / 32, kMine = TN / kChunk / 2, kBlocks = kMine * kParts32;
+        auto column_of = [&](int b) { return (2 * (b / kParts32) + group) * kChunk + (b % kParts32) * 32; };
+        uint32_t v[32], w[32];
+        tc_ld32(taddr + (uint32_t)column_of(0), w);
+#pragma unroll 1
+        for (int b = 0; b < kBlocks; ++b) {
+          const int part = b % kParts32, col0 = u.n0 + column_of(b) - 32 * part;         // first column of the chunk
+          const bool inside = col0 < p.cols && row0 < p.rows;  // the same in the whole group
+          const uint32_t buf = pre ? 0u : (n_chunk & 1u) * kChunkBytes;
+          if (part == 0 && inside) {
+            if (boss) {                                      // the buffers of this chunk have been read by their last stores
+              if (pre) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+              else asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+              if (residual) {
+                const uint32_t rb = res0 + 16u * group + (buf ? 8u : 0u);
+                mbar_arrive_expect_tx(rb, kChunkBytes);
+                tma_load_3d(stage_s + buf, &maps.residual, rb, col0, row0, 0);
               }
             }
+            if (kFwd && p.bias != nullptr && t < kChunk) bias_g[t] = col0 + t < p.cols ? p.bias[col0 + t] : 0.f;
+            __syncwarp();
+            if (residual) {
+              const uint32_t bit = buf ? 2u : 1u;
+              ok = mbar_wait_warp(res0 + 16u * group + (buf ? 8u : 0u), (res_phase & bit) ? 1u : 0u, abort_flag, p.status, 45);
+              res_phase ^= bit;
+            }
+            ok = group_all(group, ok);
           }
-          if (ragged) store_ragged<kOut4>(p, p.out, u.split * p.split_out + row * p.ld_out + col, col, x);
-          if constexpr (kOut4) {
-            *reinterpret_cast<float4*>(dst + (((2u * j) ^ sw) << 4)) = make_float4(x[0], x[1], x[2], x[3]);
-            *reinterpret_cast<float4*>(dst + (((2u * j + 1u) ^ sw) << 4)) = make_float4(x[4], x[5], x[6], x[7]);
-          } else {
-            *reinterpret_cast<uint4*>(dst + (((uint32_t)j ^ sw) << 4)) =
-                make_uint4(pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]), pack2_bf16(x[4], x[5]), pack2_bf16(x[6], x[7]));
+          __syncwarp();
+          wait_ld(w);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = w[i];
+          if (b + 1 < kBlocks) {
+            tc_ld32(taddr + (uint32_t)column_of(b + 1), w);
+          } else {                                           // the accumulator has been read out
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_at(aempty0 + 8u * side, 0);
+          }
+          if (!inside) continue;
+          if (!ok) continue;                                 // (leaves after this tile, with the whole group)
+          uint8_t* dst = stage_g + buf + row_off;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(v[8 * j + i]);
+            const int col = col0 + 32 * part + 8 * j;
+            const bool ragged = col + 8 > p.whole_cols && col < p.cols && row < p.rows;
+            const uint32_t piece = ((uint32_t)(4 * part + j) ^ sw) << 4;                 // bf16: this thread's 16 bytes
+            finish(x, bias_g + 32 * part + 8 * j, row, col, [&](const float* z) {
+              if (ragged) store_ragged<kOut4>(p, p.pre, row * p.ld_out + col, col, z);
+              *reinterpret_cast<uint4*>(stage_g + kChunkBytes + row_off + piece) =
+                  make_uint4(pack2_bf16(z[0], z[1]), pack2_bf16(z[2], z[3]), pack2_bf16(z[4], z[5]), pack2_bf16(z[6], z[7]));
+            });
+            if (residual) {
+              const uint4 q = *reinterpret_cast<const uint4*>(dst + piece);
+              const uint32_t ww[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                x[2 * i] += __uint_as_float(ww[i] << 16);
+                x[2 * i + 1] += __uint_as_float(ww[i] & 0xFFFF0000u);
+              }
+            }
+            if (ragged) store_ragged<kOut4>(p, p.out, u.split * p.split_out + row * p.ld_out + col, col, x);
+            if constexpr (kOut4) {
+              *reinterpret_cast<float4*>(dst + (((2u * j) ^ sw) << 4)) = make_float4(x[0], x[1], x[2], x[3]);
+              *reinterpret_cast<float4*>(dst + (((2u * j + 1u) ^ sw) << 4)) = make_float4(x[4], x[5], x[6], x[7]);
+            } else {
+              *reinterpret_cast<uint4*>(dst + piece) =
+                  make_uint4(pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]), pack2_bf16(x[4], x[5]), pack2_bf16(x[6], x[7]));
+            }
+          }
+          if (part == kParts32 - 1) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            group_all(group, true);
+            if (boss && col0 < p.whole_cols) {
+              store_box(&maps.out, stage_s + buf, col0, row0, u.split);
+              if (pre) store_box(&maps.pre, stage_s + kChunkBytes, col0, row0, 0);
+              asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            }
+            ++n_chunk;
           }
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        group_all(group, true);
-        if (boss && col0 < p.whole_cols) {
-          store_box(&maps.out, stage_s + buf, col0, row0, u.split);
-          if (pre) store_box(&maps.pre, stage_s + kChunkBytes, col0, row0, 0);
-          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-        }
-        ++n_chunk;
+        ++it;
       }
-      if (kMode != kF32) ++it;
     }
     if (boss) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
@@ -560,7 +616,7 @@ int launch_kind(const DenseProduct& q, const DenseEpilogue& e, cudaStream_t st) 
   p.b = q.b.f32; p.b_si = q.b.si; p.b_sk = q.b.sk;
   const int unit = kMode == kBf16 ? 8 : 4;
   p.whole_cols = kMode == kPartial ? q.cols : q.cols / unit * unit;     // (part sums: rows padded to whole pieces)
-  p.out = q.out; p.pre = e.pre; p.ld_out = q.ld_out; p.split_out = (long long)q.rows * q.ld_out;
+  p.out = q.out; p.pre = e.pre; p.residual = e.residual; p.ld_out = q.ld_out; p.split_out = (long long)q.rows * q.ld_out;
   p.status = q.status; p.clear_status = q.clear_status ? 1 : 0;
   DenseMaps m;
   const int depth = q.f32 ? 3 : 1, elt = kMode == kBf16 ? 2 : 4;
