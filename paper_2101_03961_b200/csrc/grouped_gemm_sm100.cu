@@ -345,16 +345,16 @@ int tc::make_map(CUtensorMap* tm, const void* base, long long E, long long rows,
 }
 
 int tc::make_map_rows(CUtensorMap* tm, const void* base, int elt, long long depth, long long rows, long long cols,
-                      long long ld, int box_rows) {
+                      long long ld, int box_bytes, int box_rows) {
   EncodeTiledFn fn = get_encode_fn();
   if (fn == nullptr) return SWITCH_MOE_CUDA_ERROR;
   cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)depth};
   cuuint64_t strides[2] = {(cuuint64_t)ld * elt, (cuuint64_t)ld * (cuuint64_t)rows * elt};
-  cuuint32_t box[3] = {(cuuint32_t)(128 / elt), (cuuint32_t)box_rows, 1};
+  cuuint32_t box[3] = {(cuuint32_t)(box_bytes / elt), (cuuint32_t)box_rows, 1};
   cuuint32_t estr[3] = {1, 1, 1};
   CUresult r = fn(tm, elt == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<void*>(base),
-                  dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                  dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  box_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? SWITCH_MOE_OK : SWITCH_MOE_CUDA_ERROR;
 }
 

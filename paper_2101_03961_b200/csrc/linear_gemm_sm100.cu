@@ -3,12 +3,13 @@
 //
 // A CTA pair works on tiles of 256 x TN outputs (TN 256, or 128 where that fills the chip better); each CTA stages its own
 // 128 rows of A and half of B's columns per 64-deep block of the contraction by TMA, the leader's MMA warp issues the
-// instructions for both, and eight epilogue warps of each CTA drain its 128 accumulator lanes (a lane = an output row)
-// while the next tile's products run in the other half of tensor memory.  Four of them form a group that takes every
-// second chunk of 128 bytes of the output rows: from tensor memory through the epilogue into 128-byte-swizzled shared
-// memory, and from there by TMA, which also brings the residual's chunk into the very buffer that the result leaves from
-// and clips what is outside (a store in whole 16-byte pieces: the last columns of a row that does not end on one are
-// written element by element).
+// instructions for both, and sixteen epilogue warps of each CTA drain its 128 accumulator lanes (a lane = an output row)
+// while the next tile's products run in the other half of tensor memory.  A warp has 32 rows and a quarter of the columns,
+// and works on its own: 32 columns at a time from tensor memory through the epilogue into 64-byte-swizzled shared memory,
+// and from there by TMA, which also brings the residual into the very buffer that the result leaves from and clips what is
+// outside (a store in whole 16-byte pieces: the last columns of a row that does not end on one are written element by
+// element).  With GELU the epilogue is latency-bound (ncu: 0.30 instructions a cycle and scheduler with eight warps), hence
+// sixteen.
 //
 // Float32 operands come as three bfloat16 parts (x 2^24 = h + m + l, exact); of the nine cross products six are formed,
 // the others are below 2^-25 of the product.  The tensor pipe adds with truncation, so an accumulator lives for one block
@@ -16,7 +17,7 @@
 // Results that are not finite are formed again by fused multiply-adds from the float32 operands (operands from 2^104 on
 // and sums from 2^80 on end there too).
 //
-// Every wait is bounded in time; after one gave up all roles leave, and the threads of an epilogue group decide together.
+// Every wait is bounded in time; after one gave up all roles leave.
 #include <cmath>
 
 #include "linear_common.cuh"
@@ -26,15 +27,18 @@ namespace swmoe {
 using namespace tc;
 namespace {
 
-constexpr int kThreads = 320;                        // TMA, MMA, eight epilogue warps
+constexpr int kEpiWarps = 16;
+constexpr int kThreads = 64 + 32 * kEpiWarps;        // TMA, MMA, epilogue
 constexpr int kABlock = 16384;                       // 128 rows x 64 steps of bfloat16
-constexpr int kChunkBytes = 16384;                   // 128 rows x 128 bytes of output
-constexpr int kBuffers = 2;                          // chunks in shared memory per epilogue group
-constexpr int kStagingBytes = 2 * kBuffers * kChunkBytes;
+constexpr int kBufferBytes = 32 * 64;                // 32 rows x 64 bytes of output
+constexpr int kWarpStage = 2 * kBufferBytes;
+constexpr int kStagingBytes = kEpiWarps * kWarpStage;
 constexpr int kRingBytes = 163840;
 constexpr int kMaxRing = 8;
-constexpr int kBiasBytes = 2 * 64 * 4;
-constexpr int kSmem = 1024 + kRingBytes + kStagingBytes + kBiasBytes + 256;
+constexpr int kBiasBytes = kEpiWarps * 32 * 4;
+constexpr int kBarBytes = 512;
+constexpr int kSmem = kRingBytes + kStagingBytes + kBiasBytes + kBarBytes;
+static_assert(kSmem <= 232448, "shared memory of a block");
 constexpr uint32_t kPeer = 0xFEFFFFFFu;              // clears the CTA-rank bit of a shared::cluster address
 constexpr int kBand = 8;                             // row tiles that are walked together along the columns
 
@@ -103,16 +107,6 @@ __device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uin
       "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// Barrier of one epilogue group (128 threads); true if `ok` holds in every one of them.
-__device__ __forceinline__ bool group_all(int group, bool ok) {
-  uint32_t r;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.u32 p, %2, 0;\n\t"
-      "barrier.cta.red.and.pred q, %1, 128, p;\n\t"
-      "selp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(group + 1), "r"((uint32_t)ok) : "memory");
-  return r != 0;
-}
 // Registers pass through so that no use of them moves ahead of the wait.
 __device__ __forceinline__ void wait_ld(uint32_t* r) {
   asm volatile("tcgen05.wait::ld.sync.aligned;"
@@ -164,28 +158,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant__ DenseParams p) {
   constexpr bool kFwd = !kAMn && kBMn;                       // the only product with an epilogue of its own
   constexpr bool kOut4 = kMode != kBf16;                     // float32 output
-  constexpr int kChunk = kOut4 ? 32 : 64;                    // output columns per chunk
   constexpr int kBBlock = TN * 64;                           // this CTA's half of B: TN / 2 columns x 64 steps
   constexpr int kStage = kABlock + kBBlock;
   constexpr int kStages = kRingBytes / kStage < kMaxRing ? kRingBytes / kStage : kMaxRing;
   constexpr int kParts = kMode == kF32 ? 6 : 1;
   pdl_launch_dependents();
-  extern __shared__ uint8_t smem_raw[];
-  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
+  extern __shared__ __align__(1024) uint8_t gen[];           // (all of an SM's shared memory: no room to align it by hand)
+  const uint32_t base = smem_u32(gen);
   float* bias_s = reinterpret_cast<float*>(gen + kRingBytes + kStagingBytes);
   uint8_t* bar_gen = gen + kRingBytes + kStagingBytes + kBiasBytes;
   const uint32_t bars = base + kRingBytes + kStagingBytes + kBiasBytes;
-  // full[8] | empty[8] | acc_full[2] | acc_empty[2] | residual[2 groups x 2] | tmem | abort, progress
-  const uint32_t full0 = bars, empty0 = bars + 64u, afull0 = bars + 128u, aempty0 = bars + 144u, res0 = bars + 160u;
-  volatile uint32_t* tmem_s = reinterpret_cast<volatile uint32_t*>(bar_gen + 192);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(bar_gen + 200);
+  // full[8] | empty[8] | acc_full[2] | acc_empty[2] | tmem | abort, progress | .. | residual[16 warps x 2]
+  const uint32_t full0 = bars, empty0 = bars + 64u, afull0 = bars + 128u, aempty0 = bars + 144u, res0 = bars + 256u;
+  volatile uint32_t* tmem_s = reinterpret_cast<volatile uint32_t*>(bar_gen + 160);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bar_gen + 168);
+  const uint32_t progress = bars + 172u;
   const int warp = uniform_warp_id(), lane = threadIdx.x & 31;
   const uint32_t rank = __shfl_sync(0xffffffffu, cta_rank(), 0);
   if (threadIdx.x == 0) {
     for (int s = 0; s < kMaxRing; ++s) { mbar_init(full0 + 8u * s, 1); mbar_init(empty0 + 8u * s, 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(afull0 + 8u * a, 1); mbar_init(aempty0 + 8u * a, 16); }
-    for (int a = 0; a < 4; ++a) mbar_init(res0 + 8u * a, 1);
+    for (int a = 0; a < 2; ++a) { mbar_init(afull0 + 8u * a, 1); mbar_init(aempty0 + 8u * a, 2 * kEpiWarps); }
+    for (int a = 0; a < 2 * kEpiWarps; ++a) mbar_init(res0 + 8u * a, 1);
     abort_flag[0] = 0;
     abort_flag[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -290,17 +283,17 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
     }
   } else {
     // ------------------------------------------------------------------------------------------ epilogue (both CTAs)
-    const int lg = warp & 3, group = (warp - 2) >> 2, t = (int)threadIdx.x - 64 - 128 * group;   // t: thread of the group
+    const int lg = warp & 3, ew = warp - 2, quarter = ew >> 2;
     const int r = 32 * lg + lane;                            // this thread's row of the CTA's 128
-    const bool boss = t == 0;                                // issues the group's copies
-    const uint32_t stage_s = base + kRingBytes + (uint32_t)(group * kBuffers * kChunkBytes);
-    uint8_t* stage_g = gen + kRingBytes + group * kBuffers * kChunkBytes;
-    float* bias_g = bias_s + 64 * group;
-    const uint32_t row_off = (uint32_t)r * 128u, sw = (uint32_t)(r & 7);
+    uint8_t* stage_g = gen + kRingBytes + ew * kWarpStage;
+    const uint32_t stage_s = base + kRingBytes + (uint32_t)(ew * kWarpStage);
+    float* bias_w = bias_s + 32 * ew;
+    const uint32_t res_bar = res0 + 16u * ew;
+    const uint32_t row_off = (uint32_t)lane * 64u, sw = (uint32_t)(lane >> 1) & 3u;
     const bool pre = kFwd && p.has_pre, residual = kFwd && p.has_residual;
     DropoutState rng{};
     if (kFwd) rng = dropout_state(p.dropout);
-    uint32_t it = 0, n_chunk = 0, res_phase = 0;             // res_phase: a bit per buffer
+    uint32_t it = 0, n_block = 0, res_phase = 0;             // res_phase: a bit per buffer
     bool ok = true;
     // The result of eight columns: bias, activation, dropout.  `saved` is called with z.
     auto finish = [&](float* x, const float* bias8, long long row, int col, auto&& saved) {
@@ -328,58 +321,95 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
         }
       }
     };
+    constexpr int kCols = TN / 4, kBlocks = kCols / 32;      // this warp's columns of a tile, 32 at a time
     for (int id = pair; id < n_units && ok; id += n_pairs) {
       const Unit u = decode(p, id, TN);
-      const int row0 = u.m0 + 128 * (int)rank;
-      const long long row = row0 + r;
-      if constexpr (kMode == kF32) {
-        // A group holds one half of the tile's columns.  Blocks of the contraction are added up in registers; the sums then
-        // go through shared memory two chunks of 32 columns at a time, so that what follows is a loop and not TN / 16
-        // copies of its code.
-        constexpr int kSums = TN / 2;
-        float sum[kSums];
+      const int row0 = u.m0 + 128 * (int)rank + 32 * lg, n0 = u.n0 + quarter * kCols;
+      const long long row = row0 + lane;
+      const uint32_t taddr0 = tmem + ((uint32_t)(lg * 32) << 16) + quarter * kCols;
+      float sum[kMode == kF32 ? kCols : 1];
+      if constexpr (kMode == kF32) {                         // blocks of the contraction are added up in registers
 #pragma unroll
-        for (int i = 0; i < kSums; ++i) sum[i] = 0.f;
+        for (int i = 0; i < kCols; ++i) sum[i] = 0.f;
         for (int kb = u.kb0; kb < u.kb1; ++kb, ++it) {
           const uint32_t side = it & 1u;
           ok = mbar_wait_warp<true>(afull0 + 8u * side, (it >> 1) & 1u, abort_flag, p.status, 44);
           if (!ok) break;
           tc_fence_after();
-          const uint32_t taddr = tmem + ((uint32_t)(lg * 32) << 16) + side * TN + group * (TN / 2);
 #pragma unroll
-          for (int c = 0; c < TN / 64; ++c) {
+          for (int b = 0; b < kBlocks; ++b) {
             uint32_t v[32];
-            tc_ld32(taddr + 32u * c, v);
+            tc_ld32(taddr0 + side * TN + 32u * b, v);
             wait_ld(v);
-            if (c == TN / 64 - 1) {
+            if (b == kBlocks - 1) {
               tc_fence_before();
               __syncwarp();
               if (lane == 0) arrive_at(aempty0 + 8u * side, 0);
             }
 #pragma unroll
-            for (int i = 0; i < 32; ++i) sum[32 * c + i] += __uint_as_float(v[i]);
+            for (int i = 0; i < 32; ++i) sum[32 * b + i] += __uint_as_float(v[i]);
           }
         }
-        if (!group_all(group, ok)) { ok = false; break; }
+      } else {
+        ok = mbar_wait_warp(afull0 + 8u * (it & 1u), (it >> 1) & 1u, abort_flag, p.status, 44);
+        tc_fence_after();
+      }
+      if (!ok) break;
+      // One copy of this loop's code, not one per block: unrolled, it streams through the instruction caches (32768 tokens,
+      // 768 x 2048, GELU: 199 us against 169 with eight warps).
 #pragma unroll 1
-        for (int half = 0; half < TN / 128; ++half) {
-          if (boss) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-          group_all(group, true);
+      for (int b = 0; b < kBlocks; ++b) {
+        const int col0 = n0 + 32 * b;
+        const bool inside = col0 < p.cols && row0 < p.rows;  // the same in the whole warp
+        // bf16: a block is one buffer of 64-byte rows; with pre the results use the first and z the second.  Float32: both.
+        const uint32_t buf = pre || kOut4 ? 0u : (n_block & 1u) * kBufferBytes;
+        uint32_t v[32];
+        if constexpr (kMode != kF32) tc_ld32(taddr0 + (it & 1u) * TN + 32u * b, v);
+        if (inside) {
+          if (lane == 0) {                                   // this block's buffers have been read by their last stores
+            if (pre || kOut4) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            else asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+            if (residual && !kOut4) {
+              const uint32_t rb = res_bar + (buf ? 8u : 0u);
+              mbar_arrive_expect_tx(rb, kBufferBytes);
+              tma_load_3d(stage_s + buf, &maps.residual, rb, col0, row0, 0);
+            }
+          }
+          if (kFwd && p.bias != nullptr) bias_w[lane] = col0 + lane < p.cols ? p.bias[col0 + lane] : 0.f;
+          __syncwarp();
+        }
+        if constexpr (kMode != kF32) {
+          wait_ld(v);
+          if (b == kBlocks - 1) {                            // the accumulator has been read out
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_at(aempty0 + 8u * (it & 1u), 0);
+          }
+        }
+        if (!inside) continue;
+        if (residual && !kOut4) {
+          const uint32_t bit = buf ? 2u : 1u;
+          ok = mbar_wait_warp(res_bar + (buf ? 8u : 0u), (res_phase & bit) ? 1u : 0u, abort_flag, p.status, 45);
+          res_phase ^= bit;
+          if (!ok) break;
+        }
+        uint8_t* dst = stage_g + buf + row_off;
+        auto piece_at = [&](int j) -> float4* {              // float32: 16-byte piece j (0 .. 7) of the row's 32 columns
+          return reinterpret_cast<float4*>(stage_g + (j >> 2) * kBufferBytes + row_off + (((uint32_t)(j & 3) ^ sw) << 4));
+        };
+        if constexpr (kMode == kF32) {
+          // The sums go through the staging buffers, so that the loop over them need not be unrolled.
           auto dump = [&](const float* s) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-              *reinterpret_cast<float4*>(stage_g + (i >> 3) * kChunkBytes + row_off + (((uint32_t)(i & 7) ^ sw) << 4)) =
-                  make_float4(s[4 * i], s[4 * i + 1], s[4 * i + 2], s[4 * i + 3]);
+            for (int j = 0; j < 8; ++j) *piece_at(j) = make_float4(s[4 * j], s[4 * j + 1], s[4 * j + 2], s[4 * j + 3]);
           };
-          if (TN == 128 || half == 0) dump(sum);
-          else dump(sum + (TN == 256 ? 64 : 0));
+          if (kBlocks == 1 || b == 0) dump(sum);
+          else dump(sum + (kBlocks == 1 ? 0 : 32));
 #pragma unroll 1
-          for (int j = 0; j < 8; ++j) {
-            const int col = u.n0 + group * (TN / 2) + 64 * half + 8 * j;
+          for (int j = 0; j < 4; ++j) {
+            const int col = col0 + 8 * j;
             if (col >= p.cols || row >= p.rows) break;
-            float4* at0 = reinterpret_cast<float4*>(stage_g + (j >> 2) * kChunkBytes + row_off + (((uint32_t)(2 * (j & 3)) ^ sw) << 4));
-            float4* at1 = reinterpret_cast<float4*>(stage_g + (j >> 2) * kChunkBytes + row_off + (((uint32_t)(2 * (j & 3) + 1) ^ sw) << 4));
-            const float4 lo = *at0, hi = *at1;
+            const float4 lo = *piece_at(2 * j), hi = *piece_at(2 * j + 1);
             float x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
             bool finite = true;
 #pragma unroll
@@ -400,17 +430,12 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
                 for (int n = 0; n < 8; ++n)
                   if (n == i && !isfinite(x[n])) x[n] = again;
                 for (uint32_t cta = 0; cta < 2; ++cta)       // the waiting warps of both CTAs see that work goes on
-                  store_at(bars + 204u, cta, (uint32_t)clock64());
+                  store_at(progress, cta, (uint32_t)clock64());
               }
-            }
-            float b8[8];
-            if (kFwd && p.bias != nullptr) {
-#pragma unroll
-              for (int i = 0; i < 8; ++i) b8[i] = col + i < p.cols ? p.bias[col + i] : 0.f;
             }
             const long long at = row * p.ld_out + col;
             const bool whole = col + 8 <= p.whole_cols;
-            finish(x, b8, row, col, [&](const float* z) {
+            finish(x, bias_w + 8 * j, row, col, [&](const float* z) {
               float* o = static_cast<float*>(p.pre) + at;
               if (whole) {
                 *reinterpret_cast<float4*>(o) = make_float4(z[0], z[1], z[2], z[3]);
@@ -428,82 +453,22 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
                 if (col + i < p.cols) x[i] += rs[i];
             }
             if (!whole) store_ragged<true>(p, p.out, u.split * p.split_out + at, col, x);
-            *at0 = make_float4(x[0], x[1], x[2], x[3]);
-            *at1 = make_float4(x[4], x[5], x[6], x[7]);
-          }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          group_all(group, true);
-          if (boss) {
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              const int col0 = u.n0 + group * (TN / 2) + 64 * half + 32 * c;
-              if (col0 < p.whole_cols && row0 < p.rows) store_box(&maps.out, stage_s + c * kChunkBytes, col0, row0, u.split);
-            }
-            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-          }
-        }
-      } else {
-        const uint32_t side = it & 1u;
-        ok = mbar_wait_warp(afull0 + 8u * side, (it >> 1) & 1u, abort_flag, p.status, 44);
-        if (!group_all(group, ok)) { ok = false; break; }
-        tc_fence_after();
-        const uint32_t taddr = tmem + ((uint32_t)(lg * 32) << 16) + side * TN;
-        // A group takes every second chunk, 32 columns of it at a time; the next 32 are on their way from tensor memory
-        // meanwhile.  (Loops, not copies: with the epilogue's code once per column block it streams through the
-        // instruction caches.)
-        constexpr int kParts32 = kChunk / 32, kMine = TN / kChunk / 2, kBlocks = kMine * kParts32;
-        auto column_of = [&](int b) { return (2 * (b / kParts32) + group) * kChunk + (b % kParts32) * 32; };
-        uint32_t v[32], w[32];
-        tc_ld32(taddr + (uint32_t)column_of(0), w);
-#pragma unroll 1
-        for (int b = 0; b < kBlocks; ++b) {
-          const int part = b % kParts32, col0 = u.n0 + column_of(b) - 32 * part;         // first column of the chunk
-          const bool inside = col0 < p.cols && row0 < p.rows;  // the same in the whole group
-          const uint32_t buf = pre ? 0u : (n_chunk & 1u) * kChunkBytes;
-          if (part == 0 && inside) {
-            if (boss) {                                      // the buffers of this chunk have been read by their last stores
-              if (pre) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-              else asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-              if (residual) {
-                const uint32_t rb = res0 + 16u * group + (buf ? 8u : 0u);
-                mbar_arrive_expect_tx(rb, kChunkBytes);
-                tma_load_3d(stage_s + buf, &maps.residual, rb, col0, row0, 0);
-              }
-            }
-            if (kFwd && p.bias != nullptr && t < kChunk) bias_g[t] = col0 + t < p.cols ? p.bias[col0 + t] : 0.f;
-            __syncwarp();
-            if (residual) {
-              const uint32_t bit = buf ? 2u : 1u;
-              ok = mbar_wait_warp(res0 + 16u * group + (buf ? 8u : 0u), (res_phase & bit) ? 1u : 0u, abort_flag, p.status, 45);
-              res_phase ^= bit;
-            }
-            ok = group_all(group, ok);
+            *piece_at(2 * j) = make_float4(x[0], x[1], x[2], x[3]);
+            *piece_at(2 * j + 1) = make_float4(x[4], x[5], x[6], x[7]);
           }
           __syncwarp();
-          wait_ld(w);
-#pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] = w[i];
-          if (b + 1 < kBlocks) {
-            tc_ld32(taddr + (uint32_t)column_of(b + 1), w);
-          } else {                                           // the accumulator has been read out
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) arrive_at(aempty0 + 8u * side, 0);
-          }
-          if (!inside) continue;
-          if (!ok) continue;                                 // (leaves after this tile, with the whole group)
-          uint8_t* dst = stage_g + buf + row_off;
+        } else {
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             float x[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(v[8 * j + i]);
-            const int col = col0 + 32 * part + 8 * j;
+            const int col = col0 + 8 * j;
+            const uint32_t piece = ((uint32_t)j ^ sw) << 4;   // bf16: this thread's 16 bytes
             const bool ragged = col + 8 > p.whole_cols && col < p.cols && row < p.rows;
-            const uint32_t piece = ((uint32_t)(4 * part + j) ^ sw) << 4;                 // bf16: this thread's 16 bytes
-            finish(x, bias_g + 32 * part + 8 * j, row, col, [&](const float* z) {
+            finish(x, bias_w + 8 * j, row, col, [&](const float* z) {
               if (ragged) store_ragged<kOut4>(p, p.pre, row * p.ld_out + col, col, z);
-              *reinterpret_cast<uint4*>(stage_g + kChunkBytes + row_off + piece) =
+              *reinterpret_cast<uint4*>(stage_g + kBufferBytes + row_off + piece) =
                   make_uint4(pack2_bf16(z[0], z[1]), pack2_bf16(z[2], z[3]), pack2_bf16(z[4], z[5]), pack2_bf16(z[6], z[7]));
             });
             if (residual) {
@@ -517,28 +482,27 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
             }
             if (ragged) store_ragged<kOut4>(p, p.out, u.split * p.split_out + row * p.ld_out + col, col, x);
             if constexpr (kOut4) {
-              *reinterpret_cast<float4*>(dst + (((2u * j) ^ sw) << 4)) = make_float4(x[0], x[1], x[2], x[3]);
-              *reinterpret_cast<float4*>(dst + (((2u * j + 1u) ^ sw) << 4)) = make_float4(x[4], x[5], x[6], x[7]);
+              *piece_at(2 * j) = make_float4(x[0], x[1], x[2], x[3]);
+              *piece_at(2 * j + 1) = make_float4(x[4], x[5], x[6], x[7]);
             } else {
               *reinterpret_cast<uint4*>(dst + piece) =
                   make_uint4(pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]), pack2_bf16(x[4], x[5]), pack2_bf16(x[6], x[7]));
             }
           }
-          if (part == kParts32 - 1) {
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            group_all(group, true);
-            if (boss && col0 < p.whole_cols) {
-              store_box(&maps.out, stage_s + buf, col0, row0, u.split);
-              if (pre) store_box(&maps.pre, stage_s + kChunkBytes, col0, row0, 0);
-              asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-            }
-            ++n_chunk;
-          }
         }
-        ++it;
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          if (col0 < p.whole_cols) store_box(&maps.out, stage_s + buf, col0, row0, u.split);
+          if (kOut4 && col0 + 16 < p.whole_cols) store_box(&maps.out, stage_s + kBufferBytes, col0 + 16, row0, u.split);
+          if (pre && !kOut4 && col0 < p.whole_cols) store_box(&maps.pre, stage_s + kBufferBytes, col0, row0, 0);
+          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+        ++n_block;
       }
+      if (kMode != kF32) ++it;
     }
-    if (boss) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
 
   // ---------------------------------------------------------------------------------------------- teardown
@@ -620,15 +584,15 @@ int launch_kind(const DenseProduct& q, const DenseEpilogue& e, cudaStream_t st) 
   p.status = q.status; p.clear_status = q.clear_status ? 1 : 0;
   DenseMaps m;
   const int depth = q.f32 ? 3 : 1, elt = kMode == kBf16 ? 2 : 4;
-  int rc = kAMn ? make_map_rows(&m.a, q.a.p, 2, depth, q.k, q.rows, q.a.ld, 64) : make_map_rows(&m.a, q.a.p, 2, depth, q.rows, q.k, q.a.ld, 128);
+  int rc = kAMn ? make_map_rows(&m.a, q.a.p, 2, depth, q.k, q.rows, q.a.ld, 128, 64) : make_map_rows(&m.a, q.a.p, 2, depth, q.rows, q.k, q.a.ld, 128, 128);
   if (rc == SWITCH_MOE_OK)
-    rc = kBMn ? make_map_rows(&m.b, q.b.p, 2, depth, q.k, q.cols, q.b.ld, 64) : make_map_rows(&m.b, q.b.p, 2, depth, q.cols, q.k, q.b.ld, TN / 2);
+    rc = kBMn ? make_map_rows(&m.b, q.b.p, 2, depth, q.k, q.cols, q.b.ld, 128, 64) : make_map_rows(&m.b, q.b.p, 2, depth, q.cols, q.k, q.b.ld, 128, TN / 2);
   const long long stored = kMode == kPartial ? q.ld_out : p.whole_cols > 0 ? p.whole_cols : unit;
-  if (rc == SWITCH_MOE_OK) rc = make_map_rows(&m.out, q.out, elt, q.splits, q.rows, stored, q.ld_out, 128);
+  if (rc == SWITCH_MOE_OK) rc = make_map_rows(&m.out, q.out, elt, q.splits, q.rows, stored, q.ld_out, 64, 32);
   m.pre = m.out;
   m.residual = m.out;
-  if (rc == SWITCH_MOE_OK && e.pre != nullptr) rc = make_map_rows(&m.pre, e.pre, elt, 1, q.rows, stored, q.ld_out, 128);
-  if (rc == SWITCH_MOE_OK && e.residual != nullptr) rc = make_map_rows(&m.residual, e.residual, elt, 1, q.rows, q.cols, q.ld_out, 128);
+  if (rc == SWITCH_MOE_OK && e.pre != nullptr) rc = make_map_rows(&m.pre, e.pre, elt, 1, q.rows, stored, q.ld_out, 64, 32);
+  if (rc == SWITCH_MOE_OK && e.residual != nullptr) rc = make_map_rows(&m.residual, e.residual, elt, 1, q.rows, q.cols, q.ld_out, 64, 32);
   if (rc != SWITCH_MOE_OK) return rc;
   return TN == 256 ? launch_kernel<kAMn, kBMn, 256, kMode>(m, p, st) : launch_kernel<kAMn, kBMn, 128, kMode>(m, p, st);
 }

@@ -192,9 +192,9 @@ __device__ __forceinline__ uint64_t make_smem_desc(uint32_t addr, uint32_t lbo_b
 // bf16 tensor [E][rows][cols] (cols contiguous), box {64 cols, box_rows rows, 1}, 128-byte swizzle, zero OOB fill.
 int make_map(CUtensorMap* tm, const void* base, long long E, long long rows, long long cols, int box_rows);
 // bf16 (elt 2) or float32 (elt 4) tensor [depth][rows][ld] of which each row's first `cols` elements belong to it; box of
-// 128 bytes x box_rows, 128-byte swizzle, zero OOB fill.
+// box_bytes x box_rows, a swizzle of as many bytes (128 or 64), zero OOB fill.
 int make_map_rows(CUtensorMap* tm, const void* base, int elt, long long depth, long long rows, long long cols, long long ld,
-                  int box_rows);
+                  int box_bytes, int box_rows);
 // float32 tensor [E][rows][cols], box {box_cols, box_rows, 1}, zero OOB fill; 128-byte swizzle where a box row is 128 bytes.
 int make_map_f32(CUtensorMap* tm, const void* base, long long E, long long rows, long long cols, int box_cols, int box_rows);
 
