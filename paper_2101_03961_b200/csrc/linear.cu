@@ -365,6 +365,8 @@ extern "C" int switch_moe_linear_fwd(const switch_moe_linear_config* cfg, const 
   q.a = {x, s.ldx, static_cast<const float*>(x), s.ldx, 1};
   q.b = {W, s.ldw, static_cast<const float*>(W), 1, s.ldw};
   q.out = y; q.ld_out = s.ldy; q.status = status; q.clear_status = true;
+  const DenseEpilogue e{bias, residual, pre, s.act, (int)(s.ldn / 8), dropout_params(rng, s.q, s.site)};
+  if (few_rows(s.f32, s.M)) return launch_dense_rows(kDenseFwd, q, e, st);
   if (s.f32) {
     __nv_bfloat16* xp = ws_ptr<__nv_bfloat16>(workspace, p.x_parts);
     __nv_bfloat16* wp = ws_ptr<__nv_bfloat16>(workspace, p.w_parts);
@@ -373,7 +375,6 @@ extern "C" int switch_moe_linear_fwd(const switch_moe_linear_config* cfg, const 
     q.a.p = xp; q.a.ld = s.ldk;
     q.b.p = wp; q.b.ld = s.ldn;
   }
-  const DenseEpilogue e{bias, residual, pre, s.act, (int)(s.ldn / 8), dropout_params(rng, s.q, s.site)};
   return launch_dense(kDenseFwd, q, e, st);
 }
 
@@ -403,13 +404,13 @@ extern "C" int switch_moe_linear_bwd(const switch_moe_linear_config* cfg, const 
   bool cleared = false;
   void* dz = own_dz && products ? ws_ptr<void>(workspace, p.dz) : nullptr;
   __nv_bfloat16* dz_parts = s.f32 && products ? ws_ptr<__nv_bfloat16>(workspace, p.dz_parts) : nullptr;
-  float* db_part = dbias != nullptr ? ws_ptr<float>(workspace, p.db_part) : nullptr;
+  float* db_part = dbias == nullptr || s.chunks == 1 ? dbias : ws_ptr<float>(workspace, p.db_part);   // one chunk: its sums are all
   if (dz != nullptr || dz_parts != nullptr || db_part != nullptr) {
     SWMOE_TRY(s.f32 ? launch_dz<float>(s, dy, pre, rng, dz, dz_parts, db_part, status, st)
                     : launch_dz<__nv_bfloat16>(s, dy, pre, rng, dz, dz_parts, db_part, status, st));
     cleared = true;
   }
-  if (dbias != nullptr) {
+  if (dbias != nullptr && s.chunks > 1) {
     launch_k(linear_db_kernel, dim3((unsigned)((s.N + 31) / 32)), dim3(1024), 0, st, static_cast<const float*>(db_part),
              s.chunks, s.N, s.ldn, dbias);
     SWMOE_TRY(launch_status());
@@ -422,13 +423,18 @@ extern "C" int switch_moe_linear_bwd(const switch_moe_linear_config* cfg, const 
     q.rows = s.M; q.cols = s.K; q.k = s.N; q.f32 = s.f32; q.splits = 1;
     q.a = go; q.a.si = ldg; q.a.sk = 1;
     q.b = {W, s.ldw, static_cast<const float*>(W), s.ldw, 1};
-    if (s.f32) {
-      __nv_bfloat16* wp = ws_ptr<__nv_bfloat16>(workspace, p.w_parts);
-      SWMOE_TRY(launch_parts(W, s.ldw, s.K, s.N, s.ldn, wp, st));
-      q.b.p = wp; q.b.ld = s.ldn;
-    }
     q.out = dx; q.ld_out = s.ldx; q.status = status; q.clear_status = !cleared;
-    SWMOE_TRY(launch_dense(kDenseDx, q, DenseEpilogue{}, st));
+    if (few_rows(s.f32, s.M)) {
+      q.a.p = g; q.a.ld = ldg;
+      SWMOE_TRY(launch_dense_rows(kDenseDx, q, DenseEpilogue{}, st));
+    } else {
+      if (s.f32) {
+        __nv_bfloat16* wp = ws_ptr<__nv_bfloat16>(workspace, p.w_parts);
+        SWMOE_TRY(launch_parts(W, s.ldw, s.K, s.N, s.ldn, wp, st));
+        q.b.p = wp; q.b.ld = s.ldn;
+      }
+      SWMOE_TRY(launch_dense(kDenseDx, q, DenseEpilogue{}, st));
+    }
     cleared = true;
   }
   if (dW != nullptr) {

@@ -40,6 +40,9 @@ struct DenseProduct {
 
 enum DenseKind { kDenseFwd = 0, kDenseDx = 1, kDenseDw = 2 };   // A, B k-major: yes, no; yes, yes; no, no
 
+// Forward product and dx of few rows: a kernel of their own (linear_rows.cu).
+inline bool few_rows(bool f32, long long rows) { return rows <= (f32 ? 16 : 64); }
+int launch_dense_rows(DenseKind kind, const DenseProduct& q, const DenseEpilogue& e, cudaStream_t st);
 int dense_splits(long long rows, long long cols, long long k);
 int launch_dense(DenseKind kind, const DenseProduct& q, const DenseEpilogue& e, cudaStream_t st);
 

@@ -284,7 +284,6 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
   } else {
     // ------------------------------------------------------------------------------------------ epilogue (both CTAs)
     const int lg = warp & 3, ew = warp - 2, quarter = ew >> 2;
-    const int r = 32 * lg + lane;                            // this thread's row of the CTA's 128
     uint8_t* stage_g = gen + kRingBytes + ew * kWarpStage;
     const uint32_t stage_s = base + kRingBytes + (uint32_t)(ew * kWarpStage);
     float* bias_w = bias_s + 32 * ew;

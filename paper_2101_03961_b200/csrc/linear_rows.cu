@@ -1,0 +1,390 @@
+// The dense product of few rows (a decoding step): out = x W with the whole epilogue, or dx = dz W^T, up to 64 rows of
+// bfloat16 or 16 of float32.  Such a call reads W once and little else, so it is all latency and bandwidth: a tile of the
+// tensor-core kernel (256 rows, one CTA pair per 128 columns and all of the contraction) would leave most SMs without work.
+//
+// Here a block has 64 output columns and a slice of the contraction; the blocks of the other slices form a cluster with it
+// and add their sums up through distributed shared memory, in rank order.  64-deep pieces of W and x come in by cp.async,
+// up to kStages at a time.  bfloat16: warp-level MMAs (16 columns of W x 8 rows of x x 16 steps: with so few rows a
+// tcgen05 tile would be padding, and the loads bound it in either case); float32: fused multiply-adds.
+// One token, 768 x 2048, GELU: 3.1 MB of weights.
+#include "linear_common.cuh"
+
+namespace swmoe {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kCols = 64, kDepth = 64;               // output columns of a block; steps per stage
+constexpr int kMaxSlices = 8;
+constexpr int kPad = kCols + 4;                      // floats between rows of the sums
+
+struct RowsParams {
+  const void* x; const void* W;
+  long long ldx, ldw, ld_out;
+  int M, N;                        // rows, output columns
+  long long K;
+  int slices, depth_per_slice;     // in stages of kDepth
+  DenseEpilogue e;
+  void* out;
+  int* status;
+};
+
+__device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// 16 bytes of which the first `bytes` are read and the rest are zeros.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void ldm4(uint32_t addr, uint32_t* r) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldm4_trans(uint32_t addr, uint32_t* r) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma16816(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float4 remote4(uint32_t local, uint32_t cta) {
+  float4 v;
+  asm volatile("{\n\t.reg .b32 ra;\n\tmapa.shared::cluster.u32 ra, %4, %5;\n\t"
+               "ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [ra];\n\t}"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(local), "r"(cta) : "memory");
+  return v;
+}
+
+// Eight results of a row: everything after the product.
+template <typename ET>
+__device__ __forceinline__ void finish8(const RowsParams& p, const DropoutState& rng, long long row, int col, float* x) {
+  const int n = min(8, p.N - col);
+  const long long at = row * p.ld_out + col;
+  auto put = [&](void* base, const float* v) {
+    ET* o = static_cast<ET*>(base) + at;
+    if constexpr (sizeof(ET) == 2) {
+      if (n == 8) {
+        __nv_bfloat162 h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        *reinterpret_cast<uint4*>(o) = *reinterpret_cast<const uint4*>(h);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < n) o[i] = __float2bfloat16(v[i]);
+      }
+    } else {
+      if (n == 8) {
+        *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
+        *reinterpret_cast<float4*>(o + 4) = make_float4(v[4], v[5], v[6], v[7]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < n) o[i] = v[i];
+      }
+    }
+  };
+  if (p.e.bias != nullptr) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] += i < n ? p.e.bias[col + i] : 0.f;
+  }
+  if (p.e.pre != nullptr) put(p.e.pre, x);
+  if (p.e.activation == SWITCH_MOE_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = x[i] < 0.f ? 0.f : x[i];
+  } else if (p.e.activation == SWITCH_MOE_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) gelu_pair(x + i, x + i + 1);
+  }
+  if (p.e.dropout.rng != nullptr) {
+    const uint4 bits = dropout_bits(p.e.dropout, rng, (unsigned long long)row * (unsigned)p.e.dropout_blocks + (unsigned)(col >> 3));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float f = dropout_factor(p.e.dropout, bits, i);
+      x[i] = f != 0.f ? x[i] * f : 0.f;
+    }
+  }
+  if (p.e.residual != nullptr) {
+    const ET* r = static_cast<const ET*>(p.e.residual) + at;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) x[i] += (float)r[i];
+  }
+  put(p.out, x);
+}
+
+// The sums of this block lie in `sums` [M][kPad]; the cluster's blocks share the rows x 8 groups of eight columns out.
+template <typename ET>
+__device__ __forceinline__ void join_slices(const RowsParams& p, const float* sums, int rank, int col0) {
+  const DropoutState rng = dropout_state(p.e.dropout);
+  const uint32_t base = smem_at(sums);
+  if (p.slices > 1) cluster_sync();
+  else __syncthreads();
+  for (int u = rank * kThreads + threadIdx.x; u < 8 * p.M; u += p.slices * kThreads) {
+    const int row = u >> 3, col = col0 + (u & 7) * 8;
+    if (col >= p.N) continue;
+    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const uint32_t at = base + (uint32_t)(row * kPad + (u & 7) * 8) * 4u;
+    for (int s = 0; s < p.slices; ++s) {
+      const float4 a = remote4(at, s), b = remote4(at + 16u, s);
+      x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w;
+      x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
+    }
+    finish8<ET>(p, rng, row, col, x);
+  }
+  if (p.slices > 1) cluster_sync();                   // no block leaves while another still reads its sums
+}
+
+// kNK: W is stored [output column][contraction] (dx), else [contraction][output column].  NT: tiles of eight rows of x.
+template <bool kNK, int NT>
+__global__ void __launch_bounds__(kThreads)
+linear_rows_kernel(const RowsParams p) {
+  constexpr int kWBytes = kCols * kDepth * 2, kXBytes = NT * 8 * kDepth * 2, kStage = kWBytes + kXBytes;
+  constexpr int kStages = 6;
+  pdl_launch_dependents();
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = blockIdx.x % p.slices, col0 = (int)(blockIdx.x / p.slices) * kCols;
+  const int first = rank * p.depth_per_slice;
+  const int total = (int)((p.K + kDepth - 1) / kDepth), count = max(0, min(p.depth_per_slice, total - first));
+  const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(p.x);
+  const __nv_bfloat16* W = static_cast<const __nv_bfloat16*>(p.W);
+  pdl_wait();
+  if (p.status != nullptr && blockIdx.x == 0 && threadIdx.x < kStatusWords) p.status[threadIdx.x] = 0;
+  // Tiles have rows of 128 bytes, their 16-byte pieces exchanged by the row.
+  auto fetch = [&](int s) {
+    const long long k0 = (long long)(first + s) * kDepth;
+    const uint32_t w_dst = smem_at(smem) + (uint32_t)(s % kStages) * kStage, x_dst = w_dst + kWBytes;
+#pragma unroll
+    for (int i = 0; i < kCols * 8 / kThreads; ++i) {
+      const int at = threadIdx.x + i * kThreads, r = at >> 3, piece = at & 7;
+      const long long outer = kNK ? (long long)col0 + r : k0 + r, inner = (kNK ? k0 : (long long)col0) + piece * 8;
+      const long long outer_end = kNK ? p.N : p.K, inner_end = kNK ? p.K : p.N;
+      const long long left = outer < outer_end ? inner_end - inner : 0;
+      const int bytes = left >= 8 ? 16 : left > 0 ? (int)left * 2 : 0;
+      copy16(w_dst + r * 128 + ((piece ^ (r & 7)) << 4), bytes > 0 ? W + outer * p.ldw + inner : W, bytes);
+    }
+    for (int at = threadIdx.x; at < NT * 64; at += kThreads) {
+      const int r = at >> 3, piece = at & 7;
+      const long long k = k0 + piece * 8, left = r < p.M ? p.K - k : 0;
+      const int bytes = left >= 8 ? 16 : left > 0 ? (int)left * 2 : 0;
+      copy16(x_dst + r * 128 + ((piece ^ (r & 7)) << 4), bytes > 0 ? x + r * p.ldx + k : x, bytes);
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s) {
+    if (s < count) fetch(s);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  // warp = 16 columns x half of a stage's steps
+  const int cg = warp & 3, kh = warp >> 2;
+  float acc[NT][4];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[t][i] = 0.f;
+  for (int s = 0; s < count; ++s) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+    __syncthreads();                                  // stage s is there, and stage s - 1 has been used by all
+    if (s + kStages - 1 < count) fetch(s + kStages - 1);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    const uint32_t w_src = smem_at(smem) + (uint32_t)(s % kStages) * kStage, x_src = w_src + kWBytes;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      const int step = 2 * kh + ks;                   // 16 steps of the contraction: pieces 2 step and 2 step + 1 of x's rows
+      uint32_t a[4];
+      if (kNK) {
+        const int r = 16 * cg + (lane & 15), piece = 2 * step + (lane >> 4);
+        ldm4(w_src + r * 128 + ((piece ^ (r & 7)) << 4), a);
+      } else {
+        const int r = 16 * step + (lane & 7) + ((lane >> 4) << 3), piece = 2 * cg + ((lane >> 3) & 1);
+        ldm4_trans(w_src + r * 128 + ((piece ^ (r & 7)) << 4), a);
+      }
+      if constexpr (NT == 1) {
+        uint32_t b[4];                                // (two of the four matrices are the same)
+        const int r = lane & 7, piece = 2 * step + ((lane >> 3) & 1);
+        ldm4(x_src + r * 128 + ((piece ^ (r & 7)) << 4), b);
+        mma16816(acc[0], a, b[0], b[1]);
+      } else {
+#pragma unroll
+        for (int t = 0; t < NT; t += 2) {
+          uint32_t b[4];
+          const int r = 8 * t + (lane & 7) + ((lane >> 4) << 3), piece = 2 * step + ((lane >> 3) & 1);
+          ldm4(x_src + r * 128 + ((piece ^ (r & 7)) << 4), b);
+          mma16816(acc[t], a, b[0], b[1]);
+          mma16816(acc[t + 1], a, b[2], b[3]);
+        }
+      }
+    }
+  }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  __syncthreads();                                    // the stages' memory is free: the sums go there
+  float* sums = reinterpret_cast<float*>(smem);
+  const int c = 16 * cg + (lane >> 2), r = 2 * (lane & 3);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {                       // the halves of the steps, one after the other
+    if (kh == h) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float* at = sums + (8 * t + r + (i & 1)) * kPad + c + 8 * (i >> 1);
+          *at = h == 0 ? acc[t][i] : *at + acc[t][i];
+        }
+    }
+    __syncthreads();
+  }
+  join_slices<__nv_bfloat16>(p, sums, rank, col0);
+}
+
+// float32: thread = one column x a quarter of a stage's steps, MT rows in registers.
+template <bool kNK, int MT>
+__global__ void __launch_bounds__(kThreads)
+linear_rows_f32_kernel(const RowsParams p) {
+  constexpr int kWBytes = kCols * kDepth * 4, kXBytes = MT * kDepth * 4, kStage = kWBytes + kXBytes;
+  constexpr int kStages = 4;
+  pdl_launch_dependents();
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int rank = blockIdx.x % p.slices, col0 = (int)(blockIdx.x / p.slices) * kCols;
+  const int first = rank * p.depth_per_slice;
+  const int total = (int)((p.K + kDepth - 1) / kDepth), count = max(0, min(p.depth_per_slice, total - first));
+  const float* x = static_cast<const float*>(p.x);
+  const float* W = static_cast<const float*>(p.W);
+  pdl_wait();
+  if (p.status != nullptr && blockIdx.x == 0 && threadIdx.x < kStatusWords) p.status[threadIdx.x] = 0;
+  // W's tile has rows of 256 bytes, their 16-byte pieces exchanged by the row where lanes read down a column of pieces.
+  auto fetch = [&](int s) {
+    const long long k0 = (long long)(first + s) * kDepth;
+    const uint32_t w_dst = smem_at(smem) + (uint32_t)(s % kStages) * kStage, x_dst = w_dst + kWBytes;
+#pragma unroll
+    for (int i = 0; i < kCols * 16 / kThreads; ++i) {
+      const int at = threadIdx.x + i * kThreads, r = at >> 4, piece = at & 15;
+      const long long outer = kNK ? (long long)col0 + r : k0 + r, inner = (kNK ? k0 : (long long)col0) + piece * 4;
+      const long long outer_end = kNK ? p.N : p.K, inner_end = kNK ? p.K : p.N;
+      const long long left = outer < outer_end ? inner_end - inner : 0;
+      const int bytes = left >= 4 ? 16 : left > 0 ? (int)left * 4 : 0;
+      copy16(w_dst + r * 256 + ((kNK ? piece ^ (r & 15) : piece) << 4), bytes > 0 ? W + outer * p.ldw + inner : W, bytes);
+    }
+    for (int at = threadIdx.x; at < MT * 16; at += kThreads) {
+      const int r = at >> 4, piece = at & 15;
+      const long long k = k0 + piece * 4, left = r < p.M ? p.K - k : 0;
+      const int bytes = left >= 4 ? 16 : left > 0 ? (int)left * 4 : 0;
+      copy16(x_dst + r * 256 + (piece << 4), bytes > 0 ? x + r * p.ldx + k : x, bytes);
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s) {
+    if (s < count) fetch(s);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  const int c = threadIdx.x & 63, kq = threadIdx.x >> 6;
+  float acc[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) acc[m] = 0.f;
+  for (int s = 0; s < count; ++s) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+    __syncthreads();
+    if (s + kStages - 1 < count) fetch(s + kStages - 1);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    const uint8_t* w_src = smem + (s % kStages) * kStage;
+    const uint8_t* x_src = w_src + kWBytes;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {                     // four steps at a time
+      const int k = 16 * kq + 4 * q;
+      float w[4];
+      if (kNK) {
+        const float4 v = *reinterpret_cast<const float4*>(w_src + c * 256 + (((k >> 2) ^ (c & 15)) << 4));
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const float*>(w_src + (k + i) * 256 + c * 4);
+      }
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const float4 v = *reinterpret_cast<const float4*>(x_src + m * 256 + k * 4);
+        acc[m] = fmaf(v.x, w[0], acc[m]);
+        acc[m] = fmaf(v.y, w[1], acc[m]);
+        acc[m] = fmaf(v.z, w[2], acc[m]);
+        acc[m] = fmaf(v.w, w[3], acc[m]);
+      }
+    }
+  }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  __syncthreads();
+  float* sums = reinterpret_cast<float*>(smem);
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    if (kq == h) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m) sums[m * kPad + c] = h == 0 ? acc[m] : sums[m * kPad + c] + acc[m];
+    }
+    __syncthreads();
+  }
+  join_slices<float>(p, sums, rank, col0);
+}
+
+template <typename Kern>
+int launch(Kern kernel, size_t smem, int slices, const RowsParams& p, bool* ready, cudaStream_t st) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return SWITCH_MOE_CUDA_ERROR;
+  if (dev < 0 || dev >= 64 || !ready[dev]) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return SWITCH_MOE_CUDA_ERROR;
+    if (dev >= 0 && dev < 64) ready[dev] = true;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(((p.N + (long long)kCols - 1) / kCols) * slices));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)slices;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  if (cudaLaunchKernelEx(&cfg, kernel, p) != cudaSuccess) launch_failed_flag() = true;
+  return launch_status();
+}
+
+template <bool kNK, int NT>
+int launch_bf16(const RowsParams& p, cudaStream_t st) {
+  static bool ready[64] = {false};
+  return launch(linear_rows_kernel<kNK, NT>, (size_t)6 * (kCols * kDepth * 2 + NT * 8 * kDepth * 2), p.slices, p, ready, st);
+}
+template <bool kNK, int MT>
+int launch_f32(const RowsParams& p, cudaStream_t st) {
+  static bool ready[64] = {false};
+  return launch(linear_rows_f32_kernel<kNK, MT>, (size_t)4 * (kCols * kDepth * 4 + MT * kDepth * 4), p.slices, p, ready, st);
+}
+template <bool kNK>
+int launch_any(const DenseProduct& q, const RowsParams& p, cudaStream_t st) {
+  if (q.f32) return q.rows <= 4 ? launch_f32<kNK, 4>(p, st) : launch_f32<kNK, 16>(p, st);
+  if (q.rows <= 8) return launch_bf16<kNK, 1>(p, st);
+  if (q.rows <= 16) return launch_bf16<kNK, 2>(p, st);
+  return q.rows <= 32 ? launch_bf16<kNK, 4>(p, st) : launch_bf16<kNK, 8>(p, st);
+}
+
+}  // namespace
+
+// `q.a.p` and `q.b.p` are the operands themselves, also of float32.  Slices: as many as fill the SMs about twice over, each
+// of at least one stage, so that none is without work.
+int launch_dense_rows(DenseKind kind, const DenseProduct& q, const DenseEpilogue& e, cudaStream_t st) {
+  RowsParams p{};
+  p.x = q.a.p; p.W = q.b.p; p.ldx = q.a.ld; p.ldw = q.b.ld; p.ld_out = q.ld_out;
+  p.M = q.rows; p.N = q.cols; p.K = q.k; p.e = e; p.out = q.out;
+  p.status = q.clear_status ? q.status : nullptr;
+  const long long blocks = ((long long)q.cols + kCols - 1) / kCols, stages = ((long long)q.k + kDepth - 1) / kDepth;
+  long long slices = 2 * kChipSms / blocks;
+  if (slices > kMaxSlices) slices = kMaxSlices;
+  if (slices > stages) slices = stages;
+  if (slices < 1) slices = 1;
+  p.depth_per_slice = (int)((stages + slices - 1) / slices);
+  p.slices = (int)((stages + p.depth_per_slice - 1) / p.depth_per_slice);
+  if (blocks * p.slices > 0x7fffffffll) return SWITCH_MOE_UNSUPPORTED_SHAPE;
+  return kind == kDenseDx ? launch_any<true>(q, p, st) : launch_any<false>(q, p, st);
+}
+
+}  // namespace swmoe

@@ -343,53 +343,69 @@ def make_balance_config(T, E, k=1, groups=1, alpha=0.01, dtype=F32, ld=0) -> Bal
 
 
 _TORCH_TYPES = {BF16: torch.bfloat16, F32: torch.float32}
+_RNG_TYPES = (torch.int64, torch.uint64)
+_MASK_TYPES = (torch.uint8, torch.bool)
+_FLOAT, _INT = (torch.float32,), (torch.int32,)
 
 
 def _refuse(where: str, name: str, why: str):
     raise SwitchMoeError(INVALID_ARGUMENT, f"{where}: {name} {why}")
 
 
+# A call's host time is most of a small call's time, so a check that passes is a few attribute reads (0.5 us a tensor); what
+# did not fit is worked out only to be reported.
 def _matrix(where, name, t, dtype, rows, cols, ld):
     """Pointer of a [rows, cols] tensor with `ld` elements between rows (0: cols), or of None."""
-    if t is None or isinstance(t, int):
+    if t is None or t.__class__ is int:
         return t
-    if t.dtype != _TORCH_TYPES.get(dtype):
-        _refuse(where, name, f"is {t.dtype}")
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+    if t.dtype is dtype and t.shape == (rows, cols) and t.get_device() == _current_device():
+        s = t.stride()
+        if (s[0] == (ld or cols) or rows <= 1) and (s[1] == 1 or cols == 1):
+            return t.data_ptr()
+    if t.dtype is not dtype:
+        _refuse(where, name, f"is {t.dtype}, not {dtype}")
+    if t.shape != (rows, cols):
         _refuse(where, name, f"is {tuple(t.shape)}, not {(rows, cols)}")
-    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) != (ld or cols)):
-        _refuse(where, name, f"has strides {t.stride()}, not {(ld or cols, 1)}")
-    return _on_device(where, name, t)
+    _check_device(where, name, t)
+    _refuse(where, name, f"has strides {t.stride()}, not {(ld or cols, 1)}")
 
 
-def _vector(where, name, t, dtype, n):
+def _vector(where, name, t, dtypes, n):
     """Pointer of a contiguous tensor of n elements, or of None."""
-    if t is None or isinstance(t, int):
+    if t is None or t.__class__ is int:
         return t
-    if t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
+    if t.dtype in dtypes and t.numel() == n and t.is_contiguous() and t.get_device() == _current_device():
+        return t.data_ptr()
+    if t.dtype not in dtypes:
         _refuse(where, name, f"is {t.dtype}")
     if t.numel() != n or not t.is_contiguous():
         _refuse(where, name, f"is {tuple(t.shape)} with strides {t.stride()}, not {n} contiguous elements")
-    return _on_device(where, name, t)
-
-
-def _on_device(where, name, t):
-    if not t.is_cuda:
-        _refuse(where, name, "is not on a GPU")
-    if t.device.index != (_device() if _device is not None else torch.cuda.current_device()):
-        _refuse(where, name, "is not on the current device")
-    return t.data_ptr()
-
-
-_RNG_TYPES = (torch.int64, torch.uint64)
+    _check_device(where, name, t)
 
 
 def _workspace_args(where, t):
     if t is None:
         return None, 0
-    if not t.is_contiguous():
-        _refuse(where, "workspace", "is not contiguous")
-    return _on_device(where, "workspace", t), t.numel() * t.element_size()
+    if t.is_contiguous() and t.get_device() == _current_device():
+        return t.data_ptr(), t.nbytes
+    _check_device(where, "workspace", t)
+    _refuse(where, "workspace", "is not contiguous")
+
+
+def _current_device() -> int:
+    if _device is None:
+        return torch.cuda.current_device() if torch.cuda.is_available() else -2
+    try:
+        return _device()
+    except RuntimeError:                                    # no driver: no tensor is on a GPU
+        return -2
+
+
+def _check_device(where, name, t):
+    if not t.is_cuda:
+        _refuse(where, name, "is not on a GPU")
+    if t.get_device() != _current_device():
+        _refuse(where, name, "is not on the current device")
 
 
 def switch_moe_linear_workspace_bytes(cfg: LinearConfig, backward=False) -> int:
@@ -423,24 +439,22 @@ def allocate_balance_workspace(cfg: BalanceConfig, device="cuda") -> torch.Tenso
 def switch_moe_linear_fwd(cfg, x, W, bias, residual, rng, y, pre, workspace, stream=None) -> None:
     """x [M, K], W [K, N], bias float32 [N] or None, residual [M, N] or None, rng int64 [2] {key, offset} (None without
     dropout); writes y [M, N] and, unless it is None, pre [M, N]."""
-    f, c = "switch_moe_linear_fwd", cfg
-    args = (_matrix(f, "x", x, c.dtype, c.M, c.K, c.ldx), _matrix(f, "W", W, c.dtype, c.K, c.N, c.ldw),
-            _vector(f, "bias", bias, torch.float32, c.N), _matrix(f, "residual", residual, c.dtype, c.M, c.N, c.ldy),
-            _vector(f, "rng", rng, _RNG_TYPES, 2), _matrix(f, "y", y, c.dtype, c.M, c.N, c.ldy),
-            _matrix(f, "pre", pre, c.dtype, c.M, c.N, c.ldy))
-    _check(load_library().switch_moe_linear_fwd(ctypes.byref(cfg), *args, *_workspace_args(f, workspace), _stream(stream)), f)
+    f, M, K, N, ldy, dt = "switch_moe_linear_fwd", cfg.M, cfg.K, cfg.N, cfg.ldy, _TORCH_TYPES.get(cfg.dtype)
+    _check((_lib or load_library()).switch_moe_linear_fwd(
+        cfg, _matrix(f, "x", x, dt, M, K, cfg.ldx), _matrix(f, "W", W, dt, K, N, cfg.ldw), _vector(f, "bias", bias, _FLOAT, N),
+        _matrix(f, "residual", residual, dt, M, N, ldy), _vector(f, "rng", rng, _RNG_TYPES, 2), _matrix(f, "y", y, dt, M, N, ldy),
+        _matrix(f, "pre", pre, dt, M, N, ldy), *_workspace_args(f, workspace), _stream(stream)), f)
 
 
 def switch_moe_linear_bwd(cfg, dy, x, W, pre, rng, workspace, dx, dW, dbias, stream=None) -> None:
     """Writes dx [M, K], dW [K, N], dbias float32 [N]; each may be None.  The residual's gradient is dy."""
-    f, c = "switch_moe_linear_bwd", cfg
-    ins = (_matrix(f, "dy", dy, c.dtype, c.M, c.N, c.ldy), _matrix(f, "x", x, c.dtype, c.M, c.K, c.ldx),
-           _matrix(f, "W", W, c.dtype, c.K, c.N, c.ldw), _matrix(f, "pre", pre, c.dtype, c.M, c.N, c.ldy),
-           _vector(f, "rng", rng, _RNG_TYPES, 2))
-    outs = (_matrix(f, "dx", dx, c.dtype, c.M, c.K, c.ldx), _matrix(f, "dW", dW, c.dtype, c.K, c.N, c.ldw),
-            _vector(f, "dbias", dbias, torch.float32, c.N))
-    _check(load_library().switch_moe_linear_bwd(ctypes.byref(cfg), *ins, *_workspace_args(f, workspace), *outs,
-                                                _stream(stream)), f)
+    f, M, K, N, ldx, ldw, ldy = "switch_moe_linear_bwd", cfg.M, cfg.K, cfg.N, cfg.ldx, cfg.ldw, cfg.ldy
+    dt = _TORCH_TYPES.get(cfg.dtype)
+    _check((_lib or load_library()).switch_moe_linear_bwd(
+        cfg, _matrix(f, "dy", dy, dt, M, N, ldy), _matrix(f, "x", x, dt, M, K, ldx), _matrix(f, "W", W, dt, K, N, ldw),
+        _matrix(f, "pre", pre, dt, M, N, ldy), _vector(f, "rng", rng, _RNG_TYPES, 2), *_workspace_args(f, workspace),
+        _matrix(f, "dx", dx, dt, M, K, ldx), _matrix(f, "dW", dW, dt, K, N, ldw), _vector(f, "dbias", dbias, _FLOAT, N),
+        _stream(stream)), f)
 
 
 def switch_moe_linear_check_device_status(cfg, workspace, stream=None) -> list:
@@ -454,37 +468,35 @@ def switch_moe_linear_check_device_status(cfg, workspace, stream=None) -> list:
 
 def switch_moe_dropout_fwd(cfg, x, residual, rng, y, stream=None) -> None:
     """y = residual + dropout(x); residual may be None, y may be x or residual."""
-    f, c = "switch_moe_dropout_fwd", cfg
-    m = lambda name, t: _matrix(f, name, t, c.dtype, c.rows, c.cols, c.ld)
-    _check(load_library().switch_moe_dropout_fwd(ctypes.byref(cfg), m("x", x), m("residual", residual),
-                                                 _vector(f, "rng", rng, _RNG_TYPES, 2), m("y", y), _stream(stream)), f)
+    f, rows, cols, ld, dt = "switch_moe_dropout_fwd", cfg.rows, cfg.cols, cfg.ld, _TORCH_TYPES.get(cfg.dtype)
+    _check((_lib or load_library()).switch_moe_dropout_fwd(
+        cfg, _matrix(f, "x", x, dt, rows, cols, ld), _matrix(f, "residual", residual, dt, rows, cols, ld),
+        _vector(f, "rng", rng, _RNG_TYPES, 2), _matrix(f, "y", y, dt, rows, cols, ld), _stream(stream)), f)
 
 
 def switch_moe_dropout_bwd(cfg, dy, rng, dx, stream=None) -> None:
     """dx = dropout(dy) with the mask of the forward call; dx may be dy."""
-    f, c = "switch_moe_dropout_bwd", cfg
-    m = lambda name, t: _matrix(f, name, t, c.dtype, c.rows, c.cols, c.ld)
-    _check(load_library().switch_moe_dropout_bwd(ctypes.byref(cfg), m("dy", dy), _vector(f, "rng", rng, _RNG_TYPES, 2),
-                                                 m("dx", dx), _stream(stream)), f)
+    f, rows, cols, ld, dt = "switch_moe_dropout_bwd", cfg.rows, cfg.cols, cfg.ld, _TORCH_TYPES.get(cfg.dtype)
+    _check((_lib or load_library()).switch_moe_dropout_bwd(
+        cfg, _matrix(f, "dy", dy, dt, rows, cols, ld), _vector(f, "rng", rng, _RNG_TYPES, 2),
+        _matrix(f, "dx", dx, dt, rows, cols, ld), _stream(stream)), f)
 
 
 def switch_moe_balance_fwd(cfg, logits, expert_index, token_mask, loss, counts, tokens, workspace, stream=None) -> None:
     """logits [T, E]; expert_index int32 [T, k] or None (the k largest logits); token_mask uint8 or bool [T] or None; writes
     loss float32 [1], counts int32 [groups, E], tokens int32 [groups]."""
-    f, c = "switch_moe_balance_fwd", cfg
-    G = c.groups or 1
-    args = (_matrix(f, "logits", logits, c.dtype, c.T, c.E, c.ld), _vector(f, "expert_index", expert_index, torch.int32, c.T * c.k),
-            _vector(f, "token_mask", token_mask, (torch.uint8, torch.bool), c.T), _vector(f, "loss", loss, torch.float32, 1),
-            _vector(f, "counts", counts, torch.int32, G * c.E), _vector(f, "tokens", tokens, torch.int32, G))
-    _check(load_library().switch_moe_balance_fwd(ctypes.byref(cfg), *args, *_workspace_args(f, workspace), _stream(stream)), f)
+    f, T, E, G = "switch_moe_balance_fwd", cfg.T, cfg.E, cfg.groups or 1
+    _check((_lib or load_library()).switch_moe_balance_fwd(
+        cfg, _matrix(f, "logits", logits, _TORCH_TYPES.get(cfg.dtype), T, E, cfg.ld),
+        _vector(f, "expert_index", expert_index, _INT, T * cfg.k), _vector(f, "token_mask", token_mask, _MASK_TYPES, T),
+        _vector(f, "loss", loss, _FLOAT, 1), _vector(f, "counts", counts, _INT, G * E), _vector(f, "tokens", tokens, _INT, G),
+        *_workspace_args(f, workspace), _stream(stream)), f)
 
 
 def switch_moe_balance_bwd(cfg, logits, token_mask, counts, tokens, d_loss, dlogits, stream=None) -> None:
     """dlogits [T, E] from the counts and tokens of the forward call; dlogits may be logits."""
-    f, c = "switch_moe_balance_bwd", cfg
-    G = c.groups or 1
-    _check(load_library().switch_moe_balance_bwd(
-        ctypes.byref(cfg), _matrix(f, "logits", logits, c.dtype, c.T, c.E, c.ld),
-        _vector(f, "token_mask", token_mask, (torch.uint8, torch.bool), c.T), _vector(f, "counts", counts, torch.int32, G * c.E),
-        _vector(f, "tokens", tokens, torch.int32, G), float(d_loss),
-        _matrix(f, "dlogits", dlogits, c.dtype, c.T, c.E, c.ld), _stream(stream)), f)
+    f, T, E, G, ld, dt = "switch_moe_balance_bwd", cfg.T, cfg.E, cfg.groups or 1, cfg.ld, _TORCH_TYPES.get(cfg.dtype)
+    _check((_lib or load_library()).switch_moe_balance_bwd(
+        cfg, _matrix(f, "logits", logits, dt, T, E, ld), _vector(f, "token_mask", token_mask, _MASK_TYPES, T),
+        _vector(f, "counts", counts, _INT, G * E), _vector(f, "tokens", tokens, _INT, G), float(d_loss),
+        _matrix(f, "dlogits", dlogits, dt, T, E, ld), _stream(stream)), f)

@@ -127,6 +127,19 @@ def test_plain_product_and_gradients(shape, dtype):
 
 @gpu
 @pytest.mark.parametrize("dtype", [sm.BF16, sm.F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("M", [1, 4, 5, 8, 9, 16, 17, 32, 33, 63, 64, 65])
+@pytest.mark.parametrize("K,N", [(65, 200), (1000, 65), (2048, 24), (24, 2051)])
+def test_few_rows(M, K, N, dtype):
+    """Both sides of each limit of the kernel for few rows: odd depths and widths, one slice of the contraction and eight."""
+    c = Case(M, K, N, dtype=dtype, act=sm.ACT_GELU, residual=M % 2 == 1, rate=0.2 * (M % 3 == 0), pad=8, seed=M)
+    c.forward()
+    c.check_forward()
+    c.backward()
+    c.check_backward()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [sm.BF16, sm.F32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("act", [sm.ACT_NONE, sm.ACT_RELU, sm.ACT_GELU], ids=["none", "relu", "gelu"])
 @pytest.mark.parametrize("residual,rate", [(False, 0.0), (True, 0.0), (False, 0.4), (True, 0.1)])
 @pytest.mark.parametrize("shape", [(1, 64, 72), (33, 40, 203), (300, 136, 392), (5, 256, 24)], ids=lambda s: "x".join(map(str, s)))
