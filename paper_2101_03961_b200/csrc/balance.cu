@@ -132,9 +132,9 @@ struct Row {
       }
     }
   }
-  // p = the softmax; returns whether the row counts (some logit is not -infinity).  A NaN anywhere, or +infinity, makes the
+  // p . scale = the softmax; returns whether the row counts (some logit is not -infinity).  A NaN anywhere, or +infinity, makes the
   // row's probabilities NaN, as in the definition: through the sum, which only a row without a finite maximum does not show.
-  __device__ __forceinline__ bool softmax(int L, float* p, float* max_out) const {
+  __device__ __forceinline__ bool softmax(int L, float* p, float* scale_out, float* max_out) const {
     float m = -INFINITY;
 #pragma unroll
     for (int i = 0; i < V * NV; ++i) m = fmaxf(m, x[i]);
@@ -148,13 +148,15 @@ struct Row {
       nan = lane_or(nan, L);
       counts = m != -INFINITY || nan != 0;
     }
+    // exp(x - m) = 2^((x - m) log2 e): the argument's rounding is 2^-24 of up to 30, the unit's error 2^-22
     float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < V * NV; ++i) { p[i] = expf(x[i] - m); s += p[i]; }
+    for (int i = 0; i < V * NV; ++i) {
+      asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(p[i]) : "f"((x[i] - m) * 1.44269504f));
+      s += p[i];
+    }
     s = lane_sum(s, L);
-    const float r = 1.f / s;
-#pragma unroll
-    for (int i = 0; i < V * NV; ++i) p[i] *= r;
+    *scale_out = 1.f / s;
     return counts;
   }
 };
@@ -193,40 +195,56 @@ balance_rows_kernel(const ET* logits, const int* index, const uint8_t* mask, Bal
     const Row<ET, V, NV> raw = next;
     const bool valid = next_valid;
     if (t + stride < s.Tg) next_valid = fetch(t + stride, next);
-    float m, p[V * NV];
-    const bool used = raw.softmax(L, p, &m) && valid;
+    if (!__any_sync(0xffffffffu, valid)) continue;    // padding, mostly at the ends of sequences
+    float m, scale, p[V * NV];
+    const bool used = raw.softmax(L, p, &scale, &m) && valid;
     if (used) {
 #pragma unroll
-      for (int i = 0; i < V * NV; ++i) acc[i] += p[i];        // (sums beyond E are never stored)
+      for (int i = 0; i < V * NV; ++i) acc[i] = fmaf(p[i], scale, acc[i]);   // (sums beyond E are never stored)
       n += l == 0;
     }
+    auto expert_of = [&](int i) { return (l + (i / V) * L) * V + i % V; };
     if (index != nullptr) {
       if (used)
         for (int c = l; c < s.k; c += L) {
           const int e = index[(row0 + t + lane / L) * s.k + c];
           if ((unsigned)e < (unsigned)s.E) atomicAdd(&smem[e], 1);
         }
-    } else {
-      // the largest logit not yet taken, the lowest index among equals, k times
+      continue;
+    }
+    // Choices.  The k-th largest distinct logit; with no ties among the k largest the choices are the logits from it on.
+    float kth = m;
+    for (int c = 1; c < s.k; ++c) {
+      float below = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < V * NV; ++i) below = raw.x[i] < kth ? fmaxf(below, raw.x[i]) : below;
+      kth = lane_max(below, L);
+    }
+    uint32_t chosen = 0;
+#pragma unroll
+    for (int i = 0; i < V * NV; ++i) chosen |= raw.x[i] >= kth && raw.x[i] != -INFINITY ? 1u << i : 0u;
+    if (!used) chosen = 0;
+    if (__any_sync(0xffffffffu, lane_sum(__popc(chosen), L) > s.k)) {
+      // ties: the largest logit not yet taken, the lowest index among equals, k times
       uint32_t taken = 0;
       for (int c = 0; c < s.k; ++c) {
-        if (c > 0) {
-          m = -INFINITY;
+        float top = -INFINITY;
 #pragma unroll
-          for (int i = 0; i < V * NV; ++i)
-            if (!(taken >> i & 1u)) m = fmaxf(m, raw.x[i]);
-          m = lane_max(m, L);
-        }
+        for (int i = 0; i < V * NV; ++i)
+          if (!(taken >> i & 1u)) top = fmaxf(top, raw.x[i]);
+        top = lane_max(top, L);
         int best = 0x7fffffff, slot = 0;
 #pragma unroll
         for (int i = V * NV - 1; i >= 0; --i)
-          if (!(taken >> i & 1u) && raw.x[i] == m) { best = (l + (i / V) * L) * V + i % V; slot = i; }
-        const int e = lane_min(best, L);
-        if (best == e) {
-          taken |= 1u << slot;
-          if (used && m != -INFINITY && e < s.E) atomicAdd(&smem[e], 1);
-        }
+          if (!(taken >> i & 1u) && raw.x[i] == top) { best = expert_of(i); slot = i; }
+        if (lane_min(best, L) == best && top != -INFINITY) taken |= 1u << slot;
       }
+      chosen = used ? taken : 0;
+    }
+    while (chosen != 0) {
+      const int i = __ffs(chosen) - 1;
+      chosen &= chosen - 1;
+      atomicAdd(&smem[expert_of(i)], 1);
     }
   }
   // lanes with the same l of a warp, then the warps in order
@@ -272,6 +290,7 @@ balance_sum_kernel(const int* tokens_part, const int* counts_part, const float* 
   const int e = blockIdx.x * kFinalExperts + lane;
   double p = 0.0;                                     // (a group may have millions of tokens)
   int c = 0, n = 0;
+#pragma unroll 4
   for (int b = warp; b < s.blocks; b += kWarps) {
     const long long part = (long long)g * s.blocks + b;
     if (e < s.E) {
@@ -340,12 +359,17 @@ balance_bwd_kernel(const ET* logits, const uint8_t* mask, const int* counts, con
     const bool valid = at < s.Tg && (mask == nullptr || mask[row0 + at] != 0);
     Row<ET, V, NV> r;
     r.load(logits + (row0 + (valid ? at : 0)) * s.ld, valid, l, L, s.E);
-    float m, p[V * NV];
-    const bool used = r.softmax(L, p, &m) && valid;
-    float dot = 0.f;
+    float m, scale = 0.f, dot = 0.f, p[V * NV];
+    bool used = false;
+    if (__any_sync(0xffffffffu, valid)) {
+      used = r.softmax(L, p, &scale, &m) && valid;
 #pragma unroll
-    for (int i = 0; i < V * NV; ++i) dot += p[i] * grad[i];
-    dot = lane_sum(dot, L);
+      for (int i = 0; i < V * NV; ++i) {
+        p[i] *= scale;
+        dot += p[i] * grad[i];
+      }
+      dot = lane_sum(dot, L);
+    }
     if (at < s.Tg) {
       ET* out = dlogits + (row0 + at) * s.ld;
 #pragma unroll

@@ -9,83 +9,112 @@ namespace {
 
 constexpr int kThreads = 256;
 
+// Eight elements in flight: loaded now, converted when they are needed.
 template <typename ET> struct Eight;
 template <> struct Eight<__nv_bfloat16> {
-  static __device__ __forceinline__ void load(const __nv_bfloat16* p, float* f) {
-    const uint4 v = *reinterpret_cast<const uint4*>(p);
-    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+  uint4 v;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void load(const __nv_bfloat16* p, int n) {
+    const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
+    uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { const float2 t = __bfloat1622float2(h[i]); f[2 * i] = t.x; f[2 * i + 1] = t.y; }
+    for (int i = 0; i < 4; ++i) w[i] = (2 * i < n ? q[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)q[2 * i + 1] << 16 : 0u);
+    v = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  __device__ __forceinline__ void get(float* f) const {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
   }
   static __device__ __forceinline__ void store(__nv_bfloat16* p, const float* f) {
-    uint4 v;
-    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
+    uint4 o;
+    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&o);
 #pragma unroll
     for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-    *reinterpret_cast<uint4*>(p) = v;
+    *reinterpret_cast<uint4*>(p) = o;
   }
+  static __device__ __forceinline__ void store1(__nv_bfloat16* p, float f) { *p = __float2bfloat16(f); }
 };
 template <> struct Eight<float> {
-  static __device__ __forceinline__ void load(const float* p, float* f) {
+  float4 lo, hi;
+  __device__ __forceinline__ void load(const float* p) {
+    lo = *reinterpret_cast<const float4*>(p);
+    hi = *reinterpret_cast<const float4*>(p + 4);
+  }
+  __device__ __forceinline__ void load(const float* p, int n) {
+    float f[8];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float4 v = *reinterpret_cast<const float4*>(p + 4 * i);
-      f[4 * i] = v.x; f[4 * i + 1] = v.y; f[4 * i + 2] = v.z; f[4 * i + 3] = v.w;
-    }
+    for (int i = 0; i < 8; ++i) f[i] = i < n ? p[i] : 0.f;
+    lo = make_float4(f[0], f[1], f[2], f[3]);
+    hi = make_float4(f[4], f[5], f[6], f[7]);
+  }
+  __device__ __forceinline__ void get(float* f) const {
+    f[0] = lo.x; f[1] = lo.y; f[2] = lo.z; f[3] = lo.w;
+    f[4] = hi.x; f[5] = hi.y; f[6] = hi.z; f[7] = hi.w;
   }
   static __device__ __forceinline__ void store(float* p, const float* f) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      *reinterpret_cast<float4*>(p + 4 * i) = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+    *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+    *reinterpret_cast<float4*>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
   }
+  static __device__ __forceinline__ void store1(float* p, float f) { *p = f; }
 };
-__device__ __forceinline__ float to_f(float v) { return v; }
-__device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ void from_f(float v, float* o) { *o = v; }
-__device__ __forceinline__ void from_f(float v, __nv_bfloat16* o) { *o = __float2bfloat16(v); }
 
-// A dropped element of x is 0 whatever it held (infinities and NaN too): the factor selects, it does not multiply.
-template <typename ET, bool kRes>
-__global__ void __launch_bounds__(kThreads)
+// kDense: rows follow each other without a gap and in whole blocks of eight.  Two blocks of eight per thread are asked for
+// before the first is worked on: with one, the loads' latency bounded the kernel (0.6 instructions a cycle and scheduler).
+template <typename ET, bool kRes, bool kDense>
+__global__ void __launch_bounds__(kThreads, sizeof(ET) == 2 ? 5 : 4)
 dropout_kernel(const ET* x, const ET* res, ET* y, long long blocks, int per_row, int cols, long long ld, DropoutParams d) {
   pdl_launch_dependents();
   pdl_wait();
+  constexpr int kAhead = 2;
   const DropoutState s = dropout_state(d);
-  const long long step = (long long)gridDim.x * kThreads;
-  for (long long b = (long long)blockIdx.x * kThreads + threadIdx.x; b < blocks; b += step) {
-    const long long row = blocks <= 0x7fffffffll ? (long long)((unsigned)b / (unsigned)per_row) : b / per_row;
-    const int col = (int)(b - row * per_row) * 8;
-    const long long at = row * ld + col;
-    float v[8], r[8];
-    const bool whole = col + 8 <= cols;
-    if (whole) {
-      Eight<ET>::load(x + at, v);
-      if (kRes) Eight<ET>::load(res + at, r);
-    } else {
+  const long long step = (long long)gridDim.x * kThreads * kAhead;
+  for (long long b0 = (long long)blockIdx.x * kThreads * kAhead + threadIdx.x; b0 < blocks; b0 += step) {
+    Eight<ET> a[kAhead], r[kAhead];
+    long long at[kAhead];
+    int n[kAhead];                                    // elements of the block that are in the row
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        v[i] = col + i < cols ? to_f(x[at + i]) : 0.f;
-        if (kRes) r[i] = col + i < cols ? to_f(res[at + i]) : 0.f;
+    for (int k = 0; k < kAhead; ++k) {
+      const long long b = b0 + k * kThreads;
+      n[k] = 0;
+      if (b >= blocks) continue;
+      if (kDense) {
+        at[k] = b * 8;
+        n[k] = 8;
+      } else {
+        const long long row = blocks <= 0x7fffffffll ? (long long)((unsigned)b / (unsigned)per_row) : b / per_row;
+        const int col = (int)(b - row * per_row) * 8;
+        at[k] = row * ld + col;
+        n[k] = min(8, cols - col);
+      }
+      if (n[k] == 8) {
+        a[k].load(x + at[k]);
+        if (kRes) r[k].load(res + at[k]);
+      } else {
+        a[k].load(x + at[k], n[k]);
+        if (kRes) r[k].load(res + at[k], n[k]);
       }
     }
-    if (d.rng != nullptr) {
-      const uint4 bits = dropout_bits(d, s, (unsigned long long)b);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float f = dropout_factor(d, bits, i);
-        v[i] = f != 0.f ? v[i] * f : 0.f;
+    for (int k = 0; k < kAhead; ++k) {
+      const long long b = b0 + k * kThreads;
+      if (b >= blocks) break;
+      float v[8];
+      a[k].get(v);
+      if (d.rng != nullptr) dropout8(d, dropout_bits(d, s, (unsigned long long)b), v);
+      if (kRes) {
+        float add[8];
+        r[k].get(add);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += add[i];
       }
-    }
-    if (kRes) {
+      if (n[k] == 8) {
+        Eight<ET>::store(y + at[k], v);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] += r[i];
-    }
-    if (whole) {
-      Eight<ET>::store(y + at, v);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (col + i < cols) from_f(v[i], y + at + i);
+        for (int i = 0; i < 8; ++i)
+          if (i < n[k]) Eight<ET>::store1(y + at[k] + i, v[i]);
+      }
     }
   }
 }
@@ -96,14 +125,16 @@ int launch(const switch_moe_dropout_config& c, const void* x, const void* res, c
   const int per_row = (int)(((long long)c.cols + 7) / 8);
   const long long blocks = (long long)c.rows * per_row, ld = c.ld > 0 ? c.ld : c.cols;
   const long long want = (blocks + kThreads - 1) / kThreads, most = (long long)sm_count_or_default() * 8;
-  const dim3 grid((unsigned)(want < most ? want : most));
+  const dim3 grid((unsigned)(want < most ? want : most));   // (a small call has a block of eight per thread, a larger one two)
   const DropoutParams d = dropout_params(rng, q, c.site);
   const ET* xt = static_cast<const ET*>(x);
   const ET* rt = static_cast<const ET*>(res);
-  if (res != nullptr)
-    launch_k(dropout_kernel<ET, true>, grid, dim3(kThreads), 0, st, xt, rt, static_cast<ET*>(y), blocks, per_row, c.cols, ld, d);
-  else
-    launch_k(dropout_kernel<ET, false>, grid, dim3(kThreads), 0, st, xt, rt, static_cast<ET*>(y), blocks, per_row, c.cols, ld, d);
+  const bool dense = ld == c.cols && c.cols % 8 == 0;
+  auto go = [&](auto kernel) {
+    launch_k(kernel, grid, dim3(kThreads), 0, st, xt, rt, static_cast<ET*>(y), blocks, per_row, c.cols, ld, d);
+  };
+  if (res != nullptr) dense ? go(dropout_kernel<ET, true, true>) : go(dropout_kernel<ET, true, false>);
+  else dense ? go(dropout_kernel<ET, false, true>) : go(dropout_kernel<ET, false, false>);
   return launch_status();
 }
 

@@ -65,10 +65,12 @@ __device__ __forceinline__ uint4 dropout_bits(const DropoutParams& d, const Drop
   return make_uint4(c0, c1, c2, c3);
 }
 
-// Factor of element i (0 .. 7) of the eight: 0 or the scale.
-__device__ __forceinline__ float dropout_factor(const DropoutParams& d, const uint4& bits, int i) {
-  const uint32_t w = i < 2 ? bits.x : i < 4 ? bits.y : i < 6 ? bits.z : bits.w;
-  return ((i & 1) ? w : w << 16) >= d.threshold ? d.scale : 0.f;
+// Eight values after dropout.  A dropped one is 0 whatever it was (an infinity or a NaN too).
+__device__ __forceinline__ void dropout8(const DropoutParams& d, const uint4& bits, float* v) {
+  const uint32_t w[4] = {bits.x, bits.y, bits.z, bits.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    v[i] = ((i & 1) ? w[i >> 1] : w[i >> 1] << 16) >= d.threshold ? v[i] * d.scale : 0.f;
 }
 #endif
 

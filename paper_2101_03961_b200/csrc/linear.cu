@@ -194,11 +194,7 @@ linear_dz_kernel(const ET* __restrict__ dy, const ET* __restrict__ pre, DzArgs a
         graw[k].get(g);
         if (a.dropout.rng != nullptr) {
           const uint4 bits = dropout_bits(a.dropout, rng, (unsigned long long)row * (unsigned)a.per_row + (unsigned)(col >> 3));
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float f = dropout_factor(a.dropout, bits, i);
-            g[i] = f != 0.f ? g[i] * f : 0.f;
-          }
+        dropout8(a.dropout, bits, g);
         }
         if (kAct != SWITCH_MOE_ACT_NONE) zraw[k].get(z);
         if (kAct == SWITCH_MOE_ACT_RELU) {

@@ -312,11 +312,7 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
         }
         if (p.dropout.rng != nullptr) {
           const uint4 bits = dropout_bits(p.dropout, rng, (unsigned long long)row * (unsigned)p.dropout_blocks + (unsigned)(col >> 3));
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float f = dropout_factor(p.dropout, bits, i);
-            x[i] = f != 0.f ? x[i] * f : 0.f;
-          }
+        dropout8(p.dropout, bits, x);
         }
       }
     };

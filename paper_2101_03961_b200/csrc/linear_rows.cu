@@ -99,11 +99,7 @@ __device__ __forceinline__ void finish8(const RowsParams& p, const DropoutState&
   }
   if (p.e.dropout.rng != nullptr) {
     const uint4 bits = dropout_bits(p.e.dropout, rng, (unsigned long long)row * (unsigned)p.e.dropout_blocks + (unsigned)(col >> 3));
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float f = dropout_factor(p.e.dropout, bits, i);
-      x[i] = f != 0.f ? x[i] * f : 0.f;
-    }
+        dropout8(p.e.dropout, bits, x);
   }
   if (p.e.residual != nullptr) {
     const ET* r = static_cast<const ET*>(p.e.residual) + at;
@@ -112,6 +108,16 @@ __device__ __forceinline__ void finish8(const RowsParams& p, const DropoutState&
       if (i < n) x[i] += (float)r[i];
   }
   put(p.out, x);
+}
+
+// What this thread's first eight results need from memory, on its way to L2 while the weights come in.
+template <typename ET>
+__device__ __forceinline__ void prefetch_epilogue(const RowsParams& p, int rank, int col0) {
+  const int u = rank * kThreads + threadIdx.x, row = u >> 3, col = col0 + (u & 7) * 8;
+  if (row >= p.M || col >= p.N) return;
+  if (p.e.bias != nullptr) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.e.bias + col));
+  if (p.e.residual != nullptr)
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const ET*>(p.e.residual) + row * p.ld_out + col));
 }
 
 // The sums of this block lie in `sums` [M][kPad]; the cluster's blocks share the rows x 8 groups of eight columns out.
@@ -126,6 +132,7 @@ __device__ __forceinline__ void join_slices(const RowsParams& p, const float* su
     if (col >= p.N) continue;
     float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     const uint32_t at = base + (uint32_t)(row * kPad + (u & 7) * 8) * 4u;
+#pragma unroll 4
     for (int s = 0; s < p.slices; ++s) {
       const float4 a = remote4(at, s), b = remote4(at + 16u, s);
       x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w;
@@ -177,6 +184,7 @@ linear_rows_kernel(const RowsParams p) {
     if (s < count) fetch(s);
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
+  prefetch_epilogue<__nv_bfloat16>(p, rank, col0);
   // warp = 16 columns x half of a stage's steps
   const int cg = warp & 3, kh = warp >> 2;
   float acc[NT][4];
@@ -278,6 +286,7 @@ linear_rows_f32_kernel(const RowsParams p) {
     if (s < count) fetch(s);
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
+  prefetch_epilogue<float>(p, rank, col0);
   const int c = threadIdx.x & 63, kq = threadIdx.x >> 6;
   float acc[MT];
 #pragma unroll
