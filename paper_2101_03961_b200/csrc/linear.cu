@@ -10,7 +10,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kColsPerBlock = 256, kRowLanes = 8;    // 32 threads x 8 columns, 8 rows side by side,
-constexpr int kRowsAhead = 4, kDzStep = kRowLanes * kRowsAhead;   // four of them per thread in flight
+constexpr int kDzStep = 4 * kRowLanes;               // four of them per thread in flight (float32: two)
 
 struct LinearShape {
   int M, K, N, act, q, site;
@@ -170,13 +170,14 @@ linear_dz_kernel(const ET* __restrict__ dy, const ET* __restrict__ pre, DzArgs a
   const long long col = (long long)blockIdx.x * kColsPerBlock + cx * 8;
   const int n = (int)(col < a.N ? (a.N - col < 8 ? a.N - col : 8) : 0);
   const DropoutState rng = dropout_state(a.dropout);
+  constexpr int kRowsAhead = sizeof(ET) == 2 ? 4 : 2;
   float acc[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) acc[i] = 0.f;
   const long long row_end = min((long long)a.M, (long long)(blockIdx.y + 1) * a.chunk_rows);
   if (n > 0) {
 #pragma unroll 1
-    for (long long row0 = (long long)blockIdx.y * a.chunk_rows + ry; row0 < row_end; row0 += kDzStep) {
+    for (long long row0 = (long long)blockIdx.y * a.chunk_rows + ry; row0 < row_end; row0 += kRowsAhead * kRowLanes) {
       Raw8<ET> graw[kRowsAhead], zraw[kRowsAhead];
 #pragma unroll
       for (int k = 0; k < kRowsAhead; ++k) {

@@ -1,7 +1,7 @@
 // The products of the dense layer on pairs of SMs (tcgen05 cta_group::2, M = 256): y = x W with bias, activation, dropout
 // and residual in its epilogue, dx = dz W^T, dW = x^T dz.
 //
-// A CTA pair works on tiles of 256 x TN outputs (TN 256, or 128 where that fills the chip better); each CTA stages its own
+// A CTA pair works on tiles of 256 x TN outputs (TN 256, or 192 or 128 where that fills the chip better); each CTA stages its own
 // 128 rows of A and half of B's columns per 64-deep block of the contraction by TMA, the leader's MMA warp issues the
 // instructions for both, and sixteen epilogue warps of each CTA drain its 128 accumulator lanes (a lane = an output row)
 // while the next tile's products run in the other half of tensor memory.  A warp has 32 rows and a quarter of the columns,
@@ -149,19 +149,16 @@ __device__ __forceinline__ Unit decode(const DenseParams& p, int id, int TN) {
   return u;
 }
 
-// Float32: which parts are multiplied, from the smallest products up (2 bits each): h.l, l.h, m.m, h.m, m.h, h.h.
-__device__ __forceinline__ int part_a(int q) { return (0x0118u >> (2 * q)) & 3; }   // 0, 2, 1, 0, 1, 0
-__device__ __forceinline__ int part_b(int q) { return (0x0052u >> (2 * q)) & 3; }   // 2, 0, 1, 1, 0, 0
-
 template <bool kAMn, bool kBMn, int TN, int kMode>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant__ DenseParams p) {
   constexpr bool kFwd = !kAMn && kBMn;                       // the only product with an epilogue of its own
   constexpr bool kOut4 = kMode != kBf16;                     // float32 output
-  constexpr int kBBlock = TN * 64;                           // this CTA's half of B: TN / 2 columns x 64 steps
-  constexpr int kStage = kABlock + kBBlock;
+  // This CTA's half of B: TN / 2 columns x 64 steps (n-major in boxes of 64 columns, of which TN = 192 uses one and a half)
+  constexpr int kBBoxes = (TN / 2 + 63) / 64, kBBytes = kBMn ? kBBoxes * kAtomBytes : TN * 64;
+  constexpr int kStage = kABlock + kBBoxes * kAtomBytes;
   constexpr int kStages = kRingBytes / kStage < kMaxRing ? kRingBytes / kStage : kMaxRing;
-  constexpr int kParts = kMode == kF32 ? 6 : 1;
+  constexpr int kParts = kMode == kF32 ? 3 : 1;              // of a block of 64 steps; a stage holds one part of A and of B
   pdl_launch_dependents();
   extern __shared__ __align__(1024) uint8_t gen[];           // (all of an SM's shared memory: no room to align it by hand)
   const uint32_t base = smem_u32(gen);
@@ -208,26 +205,25 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
 #pragma unroll 1
       for (int kb = u.kb0; kb < u.kb1 && ok; ++kb) {
 #pragma unroll 1
-        for (int q = 0; q < kParts; ++q) {
-          const int pa = kParts > 1 ? part_a(q) : 0, pb = kParts > 1 ? part_b(q) : 0;
+        for (int part = kParts - 1; part >= 0; --part) {     // low, middle, high
           ok = mbar_wait_warp<kProgress>(empty0 + 8u * stage, phase ^ 1u, abort_flag, p.status, 41);
           if (!ok) break;
           const uint32_t a_dst = base + stage * kStage, b_dst = a_dst + kABlock, fb = full0 + 8u * stage;
           const uint32_t lead = fb & kPeer;                  // both CTAs' bytes count on the leader's barrier
           const int k0 = kb * kBK;
           if (elect_one()) {
-            if (rank == 0) mbar_arrive_expect_tx(fb, 2u * kStage);
+            if (rank == 0) mbar_arrive_expect_tx(fb, 2u * (kABlock + kBBytes));
             if (kAMn) {
-              load_pair(a_dst, &maps.a, lead, am, k0, pa);
-              load_pair(a_dst + kAtomBytes, &maps.a, lead, am + 64, k0, pa);
+              load_pair(a_dst, &maps.a, lead, am, k0, part);
+              load_pair(a_dst + kAtomBytes, &maps.a, lead, am + 64, k0, part);
             } else {
-              load_pair(a_dst, &maps.a, lead, k0, am, pa);
+              load_pair(a_dst, &maps.a, lead, k0, am, part);
             }
             if (kBMn) {
-              load_pair(b_dst, &maps.b, lead, bn, k0, pb);
-              if (TN == 256) load_pair(b_dst + kAtomBytes, &maps.b, lead, bn + 64, k0, pb);
+              load_pair(b_dst, &maps.b, lead, bn, k0, part);
+              if (kBBoxes > 1) load_pair(b_dst + kAtomBytes, &maps.b, lead, bn + 64, k0, part);
             } else {
-              load_pair(b_dst, &maps.b, lead, k0, bn, pb);
+              load_pair(b_dst, &maps.b, lead, k0, bn, part);
             }
           }
           if (++stage == kStages) { stage = 0; phase ^= 1u; }
@@ -259,23 +255,55 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
             ok = mbar_wait_warp<kProgress>(aempty0 + 8u * side, ((it >> 1) & 1u) ^ 1u, abort_flag, p.status, 42);
             if (!ok) break;
             tc_fence_after();
-            d = tmem + side * TN;
+            d = tmem + side * 256u;
           }
-#pragma unroll 1
-          for (int q = 0; q < kParts; ++q) {
-            ok = mbar_wait_warp<kProgress>(full0 + 8u * stage, phase, abort_flag, p.status, 43);
-            if (!ok) break;
-            tc_fence_after();
-            const uint64_t ad = a_desc + (uint64_t)(stage * (kStage >> 4)), bd = b_desc + (uint64_t)(stage * (kStage >> 4));
-            const uint32_t acc = first && q == 0 ? 0u : 1u;
-            if (elect_one()) {
+          auto desc_at = [&](uint64_t d0, uint32_t s) { return d0 + (uint64_t)(s * (kStage >> 4)); };
+          auto multiply = [&](uint32_t sa, uint32_t sb, uint32_t acc) {      // one elected lane
+            const uint64_t ad = desc_at(a_desc, sa), bd = desc_at(b_desc, sb);
 #pragma unroll
-              for (int ks = 0; ks < kBK / kUmmaK; ++ks)
-                mma_pair(d, ad + ks * a_step, bd + ks * b_step, idesc, ks > 0 ? 1u : acc);
+            for (int ks = 0; ks < kBK / kUmmaK; ++ks)
+              mma_pair(d, ad + ks * a_step, bd + ks * b_step, idesc, ks > 0 ? 1u : acc);
+          };
+          auto arrived = [&](uint32_t s, uint32_t ph) {
+            ok = ok && mbar_wait_warp<kProgress>(full0 + 8u * s, ph, abort_flag, p.status, 43);
+            tc_fence_after();
+          };
+          if constexpr (kMode != kF32) {
+            arrived(stage, phase);
+            if (!ok) break;
+            if (elect_one()) {
+              multiply(stage, stage, first ? 0u : 1u);
               commit_pair(empty0 + 8u * stage);
-              if (done && q == kParts - 1) commit_pair(afull0 + 8u * side);
+              if (done) commit_pair(afull0 + 8u * side);
             }
             if (++stage == kStages) { stage = 0; phase ^= 1u; }
+          } else {
+            // Six of the nine part products; a part is loaded once and released after its last: the low one after half of
+            // the block, so that the next block's is there in time.  (Loaded anew for every product, 24 or 32 KB per 256
+            // or 512 cycles of the tensor pipe, L2 bounded it: 54% tensor activity.)
+            uint32_t s[3], ph[3];
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+              s[i] = stage; ph[i] = phase;
+              if (++stage == kStages) { stage = 0; phase ^= 1u; }
+            }
+            arrived(s[1], ph[1]);
+            if (!ok) break;
+            if (elect_one()) multiply(s[1], s[1], 0u);                       // m.m
+            arrived(s[0], ph[0]);
+            arrived(s[2], ph[2]);
+            if (!ok) break;
+            if (elect_one()) {
+              multiply(s[2], s[0], 1u);                                      // h.l
+              multiply(s[0], s[2], 1u);                                      // l.h
+              commit_pair(empty0 + 8u * s[0]);
+              multiply(s[2], s[1], 1u);                                      // h.m
+              multiply(s[1], s[2], 1u);                                      // m.h
+              commit_pair(empty0 + 8u * s[1]);
+              multiply(s[2], s[2], 1u);                                      // h.h
+              commit_pair(empty0 + 8u * s[2]);
+              commit_pair(afull0 + 8u * side);
+            }
           }
           if (done) ++it;
         }
@@ -316,27 +344,30 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
         }
       }
     };
-    constexpr int kCols = TN / 4, kBlocks = kCols / 32;      // this warp's columns of a tile, 32 at a time
+    // Of a tile's blocks of 32 columns this warp has every fourth: one or two.
+    constexpr int kMost = (TN / 32 + 3) / 4;
+    const int n_blocks = TN == 192 ? (quarter < 2 ? 2 : 1) : kMost;
     for (int id = pair; id < n_units && ok; id += n_pairs) {
       const Unit u = decode(p, id, TN);
-      const int row0 = u.m0 + 128 * (int)rank + 32 * lg, n0 = u.n0 + quarter * kCols;
+      const int row0 = u.m0 + 128 * (int)rank + 32 * lg, n0 = u.n0 + quarter * 32;
       const long long row = row0 + lane;
-      const uint32_t taddr0 = tmem + ((uint32_t)(lg * 32) << 16) + quarter * kCols;
-      float sum[kMode == kF32 ? kCols : 1];
+      const uint32_t taddr0 = tmem + ((uint32_t)(lg * 32) << 16) + quarter * 32;
+      float sum[kMode == kF32 ? 32 * kMost : 1];
       if constexpr (kMode == kF32) {                         // blocks of the contraction are added up in registers
 #pragma unroll
-        for (int i = 0; i < kCols; ++i) sum[i] = 0.f;
+        for (int i = 0; i < 32 * kMost; ++i) sum[i] = 0.f;
         for (int kb = u.kb0; kb < u.kb1; ++kb, ++it) {
           const uint32_t side = it & 1u;
           ok = mbar_wait_warp<true>(afull0 + 8u * side, (it >> 1) & 1u, abort_flag, p.status, 44);
           if (!ok) break;
           tc_fence_after();
 #pragma unroll
-          for (int b = 0; b < kBlocks; ++b) {
+          for (int b = 0; b < kMost; ++b) {
+            if (b >= n_blocks) break;
             uint32_t v[32];
-            tc_ld32(taddr0 + side * TN + 32u * b, v);
+            tc_ld32(taddr0 + side * 256u + 128u * b, v);
             wait_ld(v);
-            if (b == kBlocks - 1) {
+            if (b == n_blocks - 1) {
               tc_fence_before();
               __syncwarp();
               if (lane == 0) arrive_at(aempty0 + 8u * side, 0);
@@ -353,13 +384,13 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
       // One copy of this loop's code, not one per block: unrolled, it streams through the instruction caches (32768 tokens,
       // 768 x 2048, GELU: 199 us against 169 with eight warps).
 #pragma unroll 1
-      for (int b = 0; b < kBlocks; ++b) {
-        const int col0 = n0 + 32 * b;
+      for (int b = 0; b < n_blocks; ++b) {
+        const int col0 = n0 + 128 * b;
         const bool inside = col0 < p.cols && row0 < p.rows;  // the same in the whole warp
         // bf16: a block is one buffer of 64-byte rows; with pre the results use the first and z the second.  Float32: both.
         const uint32_t buf = pre || kOut4 ? 0u : (n_block & 1u) * kBufferBytes;
         uint32_t v[32];
-        if constexpr (kMode != kF32) tc_ld32(taddr0 + (it & 1u) * TN + 32u * b, v);
+        if constexpr (kMode != kF32) tc_ld32(taddr0 + (it & 1u) * 256u + 128u * b, v);
         if (inside) {
           if (lane == 0) {                                   // this block's buffers have been read by their last stores
             if (pre || kOut4) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
@@ -375,7 +406,7 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
         }
         if constexpr (kMode != kF32) {
           wait_ld(v);
-          if (b == kBlocks - 1) {                            // the accumulator has been read out
+          if (b == n_blocks - 1) {                           // the accumulator has been read out
             tc_fence_before();
             __syncwarp();
             if (lane == 0) arrive_at(aempty0 + 8u * (it & 1u), 0);
@@ -398,8 +429,8 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
 #pragma unroll
             for (int j = 0; j < 8; ++j) *piece_at(j) = make_float4(s[4 * j], s[4 * j + 1], s[4 * j + 2], s[4 * j + 3]);
           };
-          if (kBlocks == 1 || b == 0) dump(sum);
-          else dump(sum + (kBlocks == 1 ? 0 : 32));
+          if (kMost == 1 || b == 0) dump(sum);
+          else dump(sum + (kMost == 1 ? 0 : 32));
 #pragma unroll 1
           for (int j = 0; j < 4; ++j) {
             const int col = col0 + 8 * j;
@@ -549,14 +580,17 @@ int launch_kernel(const DenseMaps& m, const DenseParams& p, cudaStream_t st) {
   return launch_status();
 }
 
-// Tile width: 128 columns where that makes the last round of the pairs so much fuller that it pays (a 128-wide tile
-// takes about 0.6 of a 256-wide one's time), or where there are no more columns.
+// Tile width: the one whose rounds over the CTA pairs cost least, at 1, 0.78 and 0.58 of a 256-wide tile's time.
 int tile_columns(long long rows, long long cols, long long splits) {
-  if (cols <= 128) return 128;
   const long long pairs = kChipSms / 2, m = (rows + 255) / 256;
-  const long long wide = (m * ((cols + 255) / 256) * splits + pairs - 1) / pairs;
-  const long long slim = (m * ((cols + 127) / 128) * splits + pairs - 1) / pairs;
-  return 0.6 * (double)slim < (double)wide ? 128 : 256;
+  int best = 256;
+  double best_cost = 0;
+  for (int w = 256; w >= 128; w -= 64) {
+    const long long rounds = (m * ((cols + w - 1) / w) * splits + pairs - 1) / pairs;
+    const double cost = (double)rounds * (w == 256 ? 1.0 : w == 192 ? 0.78 : 0.58);
+    if (best_cost == 0 || cost < best_cost) { best = w; best_cost = cost; }
+  }
+  return best;
 }
 
 template <bool kAMn, bool kBMn, int kMode>
@@ -589,7 +623,8 @@ int launch_kind(const DenseProduct& q, const DenseEpilogue& e, cudaStream_t st) 
   if (rc == SWITCH_MOE_OK && e.pre != nullptr) rc = make_map_rows(&m.pre, e.pre, elt, 1, q.rows, stored, q.ld_out, 64, 32);
   if (rc == SWITCH_MOE_OK && e.residual != nullptr) rc = make_map_rows(&m.residual, e.residual, elt, 1, q.rows, q.cols, q.ld_out, 64, 32);
   if (rc != SWITCH_MOE_OK) return rc;
-  return TN == 256 ? launch_kernel<kAMn, kBMn, 256, kMode>(m, p, st) : launch_kernel<kAMn, kBMn, 128, kMode>(m, p, st);
+  if (TN == 256) return launch_kernel<kAMn, kBMn, 256, kMode>(m, p, st);
+  return TN == 192 ? launch_kernel<kAMn, kBMn, 192, kMode>(m, p, st) : launch_kernel<kAMn, kBMn, 128, kMode>(m, p, st);
 }
 
 }  // namespace

@@ -163,6 +163,18 @@ def test_many_tiles_and_a_split_contraction(shape, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [sm.BF16, sm.F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(4100, 520, 1400), (300, 1400, 2000), (4100, 1000, 520), (1500, 1160, 2000)], ids=lambda s: "x".join(map(str, s)))
+def test_tile_widths(shape, dtype):
+    """Shapes for which each of the three products takes each of the three tile widths, split or not."""
+    c = Case(*shape, dtype=dtype, act=sm.ACT_RELU, rate=0.05, seed=4)
+    c.forward()
+    c.check_forward()
+    c.backward()
+    c.check_backward()
+
+
+@gpu
 def test_float32_products_are_as_exact_as_fused_multiply_adds():
     """Against float64, in the root mean square: no worse than the library product that torch calls for float32."""
     for M, K, N in [(256, 64, 256), (256, 512, 256), (512, 4096, 256)]:
