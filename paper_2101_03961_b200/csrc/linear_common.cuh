@@ -76,51 +76,53 @@ __device__ __forceinline__ uint64_t pair_add(uint64_t a, uint64_t b) {
   return r;
 }
 
-// GELU and its derivative, two values at a time: gelu_cdf_pdf's approximation (Abramowitz and Stegun 7.1.26, Phi(-|z|) to
-// 7.5e-8) with the sign carried by |z| instead of a selection: with h = 1/2 - Phi(-|z|),
-//   GELU(z) = z / 2 + |z| h,   GELU'(z) = 1/2 + sign(z) h + z phi(z).
-// 9 issue slots and two special functions a value; the special functions (a quarter of the lanes a cycle) bound it.
-__device__ __forceinline__ void gelu_h(uint64_t z, uint64_t az, uint64_t* h, uint64_t* e) {
-  const float2 x = halves_of(pair_mul(pair_mul(z, pair_of(-0.72134752044448170f, -0.72134752044448170f)), z));
+// GELU and its derivative, two values at a time, from gelu_cdf_pdf's approximation (Abramowitz and Stegun 7.1.26, Phi(-|z|)
+// to 7.5e-8), without selections: with a = min(|z|, 64), beyond which Phi(-a) = 0, and q = -Phi(-a),
+//   GELU(z) = max(z, 0) + a q,   GELU'(z) = 1/2 + sign(z) (1/2 + q + a phi(a)).
+// min and max keep a NaN; the clamp keeps 0 . infinity out.  9 and 10 issue slots and two special functions a value.
+__device__ __forceinline__ float min_nan(float a, float b) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t pair_same(float v) { return pair_of(v, v); }
+// q without its last factor e = exp(-a^2 / 2): q = poly e.
+__device__ __forceinline__ void gelu_tail(uint64_t a, uint64_t* poly, uint64_t* e) {
+  const float2 x = halves_of(pair_mul(pair_mul(a, pair_same(-0.72134752044448170f)), a));
   float2 ex, t;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(ex.x) : "f"(x.x));
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(ex.y) : "f"(x.y));
-  constexpr float c = 0.3275911f * 0.70710678118654752f;
-  const float2 d = halves_of(pair_fma(az, pair_of(c, c), pair_of(1.f, 1.f)));
+  const float2 d = halves_of(pair_fma(a, pair_same(0.3275911f * 0.70710678118654752f), pair_same(1.f)));
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t.x) : "f"(d.x));
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t.y) : "f"(d.y));
   const uint64_t tt = pair_of(t.x, t.y);
   *e = pair_of(ex.x, ex.y);
-  constexpr float a5 = -0.5f * 1.061405429f, a4 = 0.5f * 1.453152027f, a3 = -0.5f * 1.421413741f, a2 = 0.5f * 0.284496736f,
-                  a1 = -0.5f * 0.254829592f;
-  uint64_t poly = pair_fma(pair_of(a5, a5), tt, pair_of(a4, a4));
-  poly = pair_fma(poly, tt, pair_of(a3, a3));
-  poly = pair_fma(poly, tt, pair_of(a2, a2));
-  poly = pair_fma(poly, tt, pair_of(a1, a1));
-  *h = pair_fma(pair_mul(poly, tt), *e, pair_of(0.5f, 0.5f));
+  uint64_t s = pair_fma(pair_same(-0.5f * 1.061405429f), tt, pair_same(0.5f * 1.453152027f));
+  s = pair_fma(s, tt, pair_same(-0.5f * 1.421413741f));
+  s = pair_fma(s, tt, pair_same(0.5f * 0.284496736f));
+  s = pair_fma(s, tt, pair_same(-0.5f * 0.254829592f));
+  *poly = pair_mul(s, tt);
 }
 __device__ __forceinline__ void gelu_pair(float* z0, float* z1) {
-  const uint64_t z = pair_of(*z0, *z1), az = pair_of(fabsf(*z0), fabsf(*z1));
-  uint64_t h, e;
-  gelu_h(z, az, &h, &e);
-  const float2 r = halves_of(pair_fma(az, h, pair_mul(z, pair_of(0.5f, 0.5f))));
-  // (an infinity: +inf / 2 + inf . 1/2 and -inf / 2 + inf . 1/2; the limit of the latter is 0)
-  *z0 = *z0 == -INFINITY ? 0.f : r.x;
-  *z1 = *z1 == -INFINITY ? 0.f : r.y;
+  const uint64_t a = pair_of(min_nan(fabsf(*z0), 64.f), min_nan(fabsf(*z1), 64.f));
+  uint64_t poly, e;
+  gelu_tail(a, &poly, &e);
+  const float2 r = halves_of(pair_fma(a, pair_mul(poly, e), pair_of(max_nan(*z0, 0.f), max_nan(*z1, 0.f))));
+  *z0 = r.x;
+  *z1 = r.y;
 }
 __device__ __forceinline__ float2 gelu_grad_pair(float z0, float z1) {
-  const uint64_t z = pair_of(z0, z1), az = pair_of(fabsf(z0), fabsf(z1));
-  uint64_t h, e;
-  gelu_h(z, az, &h, &e);
-  const float2 hh = halves_of(h);
-  const uint64_t sh = pair_of(copysignf(hh.x, z0), copysignf(hh.y, z1));
-  // (z phi(z) underflows to 0 long before z overflows; an infinity is held off it)
-  const uint64_t zc = pair_of(fminf(fmaxf(z0, -64.f), 64.f), fminf(fmaxf(z1, -64.f), 64.f));
-  const uint64_t cdf = pair_add(sh, pair_of(0.5f, 0.5f));
-  float2 g = halves_of(pair_fma(pair_mul(e, pair_of(0.3989422804014327f, 0.3989422804014327f)), zc, cdf));
-  if (z0 != z0) g.x = z0;                              // (fminf and fmaxf drop a NaN)
-  if (z1 != z1) g.y = z1;
-  return g;
+  const uint64_t a = pair_of(min_nan(fabsf(z0), 64.f), min_nan(fabsf(z1), 64.f));
+  uint64_t poly, e;
+  gelu_tail(a, &poly, &e);
+  // 1/2 + e (poly + a / sqrt(2 pi))
+  const float2 h = halves_of(pair_fma(e, pair_fma(a, pair_same(0.3989422804014327f), poly), pair_same(0.5f)));
+  return halves_of(pair_add(pair_of(copysignf(h.x, z0), copysignf(h.y, z1)), pair_same(0.5f)));
 }
 
 }  // namespace swmoe

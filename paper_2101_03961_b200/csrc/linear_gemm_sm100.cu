@@ -580,14 +580,19 @@ int launch_kernel(const DenseMaps& m, const DenseParams& p, cudaStream_t st) {
   return launch_status();
 }
 
-// Tile width: the one whose rounds over the CTA pairs cost least, at 1, 0.78 and 0.58 of a 256-wide tile's time.
-int tile_columns(long long rows, long long cols, long long splits) {
+// Tile width: the one whose rounds over the CTA pairs cost least.  A narrower tile costs more than its share, since A is
+// staged as before: measured 0.86 (0.80 where B is k-major and no box of it is wasted) and 0.62 of a 256-wide tile's time for
+// 192 and 128 columns.  us with 256 / 192 / 128 columns: 32768 tokens, 768 x 2048 forward 82 / 101 / 115, dx 87 / 81 / 94; 8192
+// tokens dx 25 / 21 / 23; 4100, 768 x 520 forward 11.1 / 10.9 / 10.4; 1000, 768 x 2048 10.2 / 9.6 / 8.1.  Float32, where a part
+// staged once serves two or three products: 0.75 and 0.5 (4001, 512 x 2048 forward 51 / 58 / 50, dx 84 / 72 / 56).
+int tile_columns(long long rows, long long cols, long long splits, bool k_major, bool f32) {
   const long long pairs = kChipSms / 2, m = (rows + 255) / 256;
+  const double share[3] = {1.0, f32 ? 0.75 : k_major ? 0.80 : 0.86, f32 ? 0.51 : 0.62};
   int best = 256;
   double best_cost = 0;
-  for (int w = 256; w >= 128; w -= 64) {
-    const long long rounds = (m * ((cols + w - 1) / w) * splits + pairs - 1) / pairs;
-    const double cost = (double)rounds * (w == 256 ? 1.0 : w == 192 ? 0.78 : 0.58);
+  for (int i = 0; i < 3; ++i) {
+    const int w = 256 - 64 * i;
+    const double cost = (double)((m * ((cols + w - 1) / w) * splits + pairs - 1) / pairs) * share[i];
     if (best_cost == 0 || cost < best_cost) { best = w; best_cost = cost; }
   }
   return best;
@@ -595,7 +600,7 @@ int tile_columns(long long rows, long long cols, long long splits) {
 
 template <bool kAMn, bool kBMn, int kMode>
 int launch_kind(const DenseProduct& q, const DenseEpilogue& e, cudaStream_t st) {
-  const int TN = tile_columns(q.rows, q.cols, q.splits);
+  const int TN = tile_columns(q.rows, q.cols, q.splits, !kBMn, q.f32);
   DenseParams p{};
   p.rows = q.rows; p.cols = q.cols; p.k = q.k;
   p.k_blocks = (int)(((long long)q.k + kBK - 1) / kBK);
