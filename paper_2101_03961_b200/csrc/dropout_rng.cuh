@@ -35,32 +35,36 @@ inline DropoutParams dropout_params(const uint64_t* rng, int q, int site) {
 
 #ifdef __CUDACC__
 struct DropoutState {
-  uint32_t k0, k1, o0, o1;
+  uint32_t k0[10], k1[10], o0, o1;                   // the rounds' keys; the counter's upper half
 };
 
 __device__ __forceinline__ DropoutState dropout_state(const DropoutParams& d) {
-  DropoutState s{0, 0, 0, 0};
+  unsigned long long key = 0, off = 0;
   if (d.rng != nullptr) {
-    const unsigned long long key = d.rng[0], off = d.rng[1];
-    s.k0 = (uint32_t)key; s.k1 = (uint32_t)(key >> 32);
-    s.o0 = (uint32_t)off; s.o1 = (uint32_t)(off >> 32);
+    key = d.rng[0];
+    off = d.rng[1];
   }
+  DropoutState s;
+#pragma unroll
+  for (int r = 0; r < 10; ++r) {
+    s.k0[r] = (uint32_t)key + (uint32_t)r * 0x9E3779B9u;
+    s.k1[r] = (uint32_t)(key >> 32) + (uint32_t)r * 0xBB67AE85u;
+  }
+  s.o0 = (uint32_t)off;
+  s.o1 = (uint32_t)(off >> 32);
   return s;
 }
 
 // The 128 bits of eight elements; `block` = row . ceil(columns / 8) + column / 8.
 __device__ __forceinline__ uint4 dropout_bits(const DropoutParams& d, const DropoutState& s, unsigned long long block) {
   uint32_t c0 = (uint32_t)block, c1 = (uint32_t)(block >> 32) + d.site, c2 = s.o0, c3 = s.o1;
-  uint32_t k0 = s.k0, k1 = s.k1;
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
     const unsigned long long a = (unsigned long long)c0 * 0xD2511F53u, b = (unsigned long long)c2 * 0xCD9E8D57u;
-    c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+    c0 = (uint32_t)(b >> 32) ^ c1 ^ s.k0[r];
     c1 = (uint32_t)b;
-    c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+    c2 = (uint32_t)(a >> 32) ^ c3 ^ s.k1[r];
     c3 = (uint32_t)a;
-    k0 += 0x9E3779B9u;
-    k1 += 0xBB67AE85u;
   }
   return make_uint4(c0, c1, c2, c3);
 }

@@ -347,9 +347,32 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
     // Of a tile's blocks of 32 columns this warp has every fourth: one or two.
     constexpr int kMost = (TN / 32 + 3) / 4;
     const int n_blocks = TN == 192 ? (quarter < 2 ? 2 : 1) : kMost;
+    const int row_in = 128 * (int)rank + 32 * lg, col_in = quarter * 32;     // this warp's place in a tile
+    // The residual of the block after the one at hand is asked for ahead (unless z takes the other buffer).
+    const bool ahead = residual && !pre && !kOut4;
+    auto fetch_residual = [&](uint32_t b, int c0, int r0) {  // one lane
+      const uint32_t rb = res_bar + (b ? 8u : 0u);
+      mbar_arrive_expect_tx(rb, kBufferBytes);
+      tma_load_3d(stage_s + b, &maps.residual, rb, c0, r0, 0);
+    };
+    auto fetch_after = [&](int id, int b, uint32_t buffer) { // that of the next block inside, from block b of unit id on
+      for (; id < n_units; id += n_pairs, b = 0) {
+        const Unit u = decode(p, id, TN);
+        for (; b < n_blocks; ++b)
+          if (u.n0 + col_in + 128 * b < p.cols && u.m0 + row_in < p.rows) {
+            if (lane == 0) fetch_residual(buffer, u.n0 + col_in + 128 * b, u.m0 + row_in);
+            return;
+          }
+      }
+    };
+    if (ahead) fetch_after(pair, 0, 0u);
     for (int id = pair; id < n_units && ok; id += n_pairs) {
       const Unit u = decode(p, id, TN);
-      const int row0 = u.m0 + 128 * (int)rank + 32 * lg, n0 = u.n0 + quarter * 32;
+      const int row0 = u.m0 + row_in, n0 = u.n0 + col_in;
+      float bias_r[kMost];                                   // on its way while the accumulator is awaited
+#pragma unroll
+      for (int b = 0; b < kMost; ++b)
+        bias_r[b] = kFwd && p.bias != nullptr && n0 + 128 * b + lane < p.cols ? p.bias[n0 + 128 * b + lane] : 0.f;
       const long long row = row0 + lane;
       const uint32_t taddr0 = tmem + ((uint32_t)(lg * 32) << 16) + quarter * 32;
       float sum[kMode == kF32 ? 32 * kMost : 1];
@@ -392,16 +415,13 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
         uint32_t v[32];
         if constexpr (kMode != kF32) tc_ld32(taddr0 + (it & 1u) * 256u + 128u * b, v);
         if (inside) {
-          if (lane == 0) {                                   // this block's buffers have been read by their last stores
-            if (pre || kOut4) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+          if (lane == 0) {                                   // this block's (and the next one's) buffers have been read by
+            if (pre || kOut4 || ahead) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");   // their last stores
             else asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-            if (residual && !kOut4) {
-              const uint32_t rb = res_bar + (buf ? 8u : 0u);
-              mbar_arrive_expect_tx(rb, kBufferBytes);
-              tma_load_3d(stage_s + buf, &maps.residual, rb, col0, row0, 0);
-            }
+            if (residual && !ahead && !kOut4) fetch_residual(buf, col0, row0);
           }
-          if (kFwd && p.bias != nullptr) bias_w[lane] = col0 + lane < p.cols ? p.bias[col0 + lane] : 0.f;
+          if (ahead) fetch_after(id, b + 1, buf ^ kBufferBytes);
+          if (kFwd && p.bias != nullptr) bias_w[lane] = b == 0 ? bias_r[0] : bias_r[kMost - 1];
           __syncwarp();
         }
         if constexpr (kMode != kF32) {
@@ -484,6 +504,7 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
           }
           __syncwarp();
         } else {
+          const bool edge = col0 + 32 > p.whole_cols;        // some of the block's columns belong to no whole 16 bytes
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             float x[8];
@@ -491,9 +512,9 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
             for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(v[8 * j + i]);
             const int col = col0 + 8 * j;
             const uint32_t piece = ((uint32_t)j ^ sw) << 4;   // bf16: this thread's 16 bytes
-            const bool ragged = col + 8 > p.whole_cols && col < p.cols && row < p.rows;
+            auto ragged = [&] { return edge && col + 8 > p.whole_cols && col < p.cols && row < p.rows; };
             finish(x, bias_w + 8 * j, row, col, [&](const float* z) {
-              if (ragged) store_ragged<kOut4>(p, p.pre, row * p.ld_out + col, col, z);
+              if (ragged()) store_ragged<kOut4>(p, p.pre, row * p.ld_out + col, col, z);
               *reinterpret_cast<uint4*>(stage_g + kBufferBytes + row_off + piece) =
                   make_uint4(pack2_bf16(z[0], z[1]), pack2_bf16(z[2], z[3]), pack2_bf16(z[4], z[5]), pack2_bf16(z[6], z[7]));
             });
@@ -506,7 +527,7 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
                 x[2 * i + 1] += __uint_as_float(ww[i] & 0xFFFF0000u);
               }
             }
-            if (ragged) store_ragged<kOut4>(p, p.out, u.split * p.split_out + row * p.ld_out + col, col, x);
+            if (ragged()) store_ragged<kOut4>(p, p.out, u.split * p.split_out + row * p.ld_out + col, col, x);
             if constexpr (kOut4) {
               *piece_at(2 * j) = make_float4(x[0], x[1], x[2], x[3]);
               *piece_at(2 * j + 1) = make_float4(x[4], x[5], x[6], x[7]);
