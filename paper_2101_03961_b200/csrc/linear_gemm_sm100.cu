@@ -19,6 +19,7 @@
 //
 // Every wait is bounded in time; after one gave up all roles leave.
 #include <cmath>
+#include <type_traits>
 
 #include "linear_common.cuh"
 #include "tc_common.cuh"
@@ -322,28 +323,36 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
     if (kFwd) rng = dropout_state(p.dropout);
     uint32_t it = 0, n_block = 0, res_phase = 0;             // res_phase: a bit per buffer
     bool ok = true;
-    // The result of eight columns: bias, activation, dropout.  `saved` is called with z.
-    auto finish = [&](float* x, const float* bias8, long long row, int col, auto&& saved) {
+    // Bias, then (once `saved` has been called with z) activation and dropout of C columns of this thread's row.  Step after
+    // step over all of them, not column after column: a store to shared memory between two columns would keep the second
+    // one's loads behind it, and the warps (four a scheduler) wait for their own results often enough.
+    auto finish = [&](auto count, float* x, const float* bias, long long row, int col, auto&& saved) {
+      constexpr int C = decltype(count)::value;
       if constexpr (kFwd) {
         if (p.bias != nullptr) {
-          const float4 b0 = *reinterpret_cast<const float4*>(bias8), b1 = *reinterpret_cast<const float4*>(bias8 + 4);
-          x[0] += b0.x; x[1] += b0.y; x[2] += b0.z; x[3] += b0.w;
-          x[4] += b1.x; x[5] += b1.y; x[6] += b1.z; x[7] += b1.w;
+#pragma unroll
+          for (int i = 0; i < C; i += 4) {
+            const float4 b = *reinterpret_cast<const float4*>(bias + i);
+            x[i] += b.x; x[i + 1] += b.y; x[i + 2] += b.z; x[i + 3] += b.w;
+          }
         }
         if (pre) saved(x);
         if (p.activation == SWITCH_MOE_ACT_RELU) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = x[i] < 0.f ? 0.f : x[i];          // (NaN stays)
+          for (int i = 0; i < C; ++i) x[i] = max_nan(x[i], 0.f);
         } else if (p.activation == SWITCH_MOE_ACT_GELU) {
 #pragma unroll
-          for (int i = 0; i < 8; i += 2) gelu_pair(x + i, x + i + 1);
+          for (int i = 0; i < C; i += 2) gelu_pair(x + i, x + i + 1);
         }
         if (p.dropout.rng != nullptr) {
-          const uint4 bits = dropout_bits(p.dropout, rng, (unsigned long long)row * (unsigned)p.dropout_blocks + (unsigned)(col >> 3));
-        dropout8(p.dropout, bits, x);
+          const unsigned long long block = (unsigned long long)row * (unsigned)p.dropout_blocks + (unsigned)(col >> 3);
+#pragma unroll
+          for (int i = 0; i < C / 8; ++i) dropout8(p.dropout, dropout_bits(p.dropout, rng, block + i), x + 8 * i);
         }
       }
     };
+    using eight = std::integral_constant<int, 8>;
+    using all32 = std::integral_constant<int, 32>;
     // Of a tile's blocks of 32 columns this warp has every fourth: one or two.
     constexpr int kMost = (TN / 32 + 3) / 4;
     const int n_blocks = TN == 192 ? (quarter < 2 ? 2 : 1) : kMost;
@@ -439,7 +448,7 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
           res_phase ^= bit;
           if (!ok) break;
         }
-        uint8_t* dst = stage_g + buf + row_off;
+        uint8_t* const dst = stage_g + buf + row_off;
         auto piece_at = [&](int j) -> float4* {              // float32: 16-byte piece j (0 .. 7) of the row's 32 columns
           return reinterpret_cast<float4*>(stage_g + (j >> 2) * kBufferBytes + row_off + (((uint32_t)(j & 3) ^ sw) << 4));
         };
@@ -481,7 +490,7 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
             }
             const long long at = row * p.ld_out + col;
             const bool whole = col + 8 <= p.whole_cols;
-            finish(x, bias_w + 8 * j, row, col, [&](const float* z) {
+            finish(eight{}, x, bias_w + 8 * j, row, col, [&](const float* z) {
               float* o = static_cast<float*>(p.pre) + at;
               if (whole) {
                 *reinterpret_cast<float4*>(o) = make_float4(z[0], z[1], z[2], z[3]);
@@ -504,37 +513,45 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
           }
           __syncwarp();
         } else {
-          const bool edge = col0 + 32 > p.whole_cols;        // some of the block's columns belong to no whole 16 bytes
+          const bool edge = col0 + 32 > p.whole_cols && row < p.rows;   // columns that belong to no whole 16 bytes
+          float x[32];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            float x[8];
+          for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(v[i]);
+          auto at16 = [&](uint8_t* row_at, int j) { return reinterpret_cast<uint4*>(row_at + (((uint32_t)j ^ sw) << 4)); };
+          auto put = [&](uint8_t* row_at, const float* f) {  // bf16: the row's four pieces of 16 bytes
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(v[8 * j + i]);
-            const int col = col0 + 8 * j;
-            const uint32_t piece = ((uint32_t)j ^ sw) << 4;   // bf16: this thread's 16 bytes
-            auto ragged = [&] { return edge && col + 8 > p.whole_cols && col < p.cols && row < p.rows; };
-            finish(x, bias_w + 8 * j, row, col, [&](const float* z) {
-              if (ragged()) store_ragged<kOut4>(p, p.pre, row * p.ld_out + col, col, z);
-              *reinterpret_cast<uint4*>(stage_g + kBufferBytes + row_off + piece) =
-                  make_uint4(pack2_bf16(z[0], z[1]), pack2_bf16(z[2], z[3]), pack2_bf16(z[4], z[5]), pack2_bf16(z[6], z[7]));
-            });
-            if (residual) {
-              const uint4 q = *reinterpret_cast<const uint4*>(dst + piece);
-              const uint32_t ww[4] = {q.x, q.y, q.z, q.w};
+            for (int j = 0; j < 4; ++j)
+              *at16(row_at, j) = make_uint4(pack2_bf16(f[8 * j], f[8 * j + 1]), pack2_bf16(f[8 * j + 2], f[8 * j + 3]),
+                                            pack2_bf16(f[8 * j + 4], f[8 * j + 5]), pack2_bf16(f[8 * j + 6], f[8 * j + 7]));
+          };
+          auto put_edge = [&](void* to, long long at, const float* f) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) store_ragged<kOut4>(p, to, at + 8 * j, col0 + 8 * j, f + 8 * j);
+          };
+          finish(all32{}, x, bias_w, row, col0, [&](const float* z) {
+            if (edge) put_edge(p.pre, row * p.ld_out + col0, z);
+            put(stage_g + kBufferBytes + row_off, z);
+          });
+          if (residual) {
+            uint4 q[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q[j] = *at16(dst, j);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t ww[4] = {q[j].x, q[j].y, q[j].z, q[j].w};
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                x[2 * i] += __uint_as_float(ww[i] << 16);
-                x[2 * i + 1] += __uint_as_float(ww[i] & 0xFFFF0000u);
+                x[8 * j + 2 * i] += __uint_as_float(ww[i] << 16);
+                x[8 * j + 2 * i + 1] += __uint_as_float(ww[i] & 0xFFFF0000u);
               }
             }
-            if (ragged()) store_ragged<kOut4>(p, p.out, u.split * p.split_out + row * p.ld_out + col, col, x);
-            if constexpr (kOut4) {
-              *piece_at(2 * j) = make_float4(x[0], x[1], x[2], x[3]);
-              *piece_at(2 * j + 1) = make_float4(x[4], x[5], x[6], x[7]);
-            } else {
-              *reinterpret_cast<uint4*>(dst + piece) =
-                  make_uint4(pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]), pack2_bf16(x[4], x[5]), pack2_bf16(x[6], x[7]));
-            }
+          }
+          if (edge) put_edge(p.out, u.split * p.split_out + row * p.ld_out + col0, x);
+          if constexpr (kOut4) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) *piece_at(j) = make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
+          } else {
+            put(dst, x);
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
