@@ -18,13 +18,14 @@ struct LinearShape {
   long long ldx, ldw, ldy, elt;
   long long ldn, ldk;                                // rows of N or K elements in the workspace, multiples of 8
   int chunks, chunk_rows;                            // row chunks of the dz kernel
-  int dw_splits;
+  DenseTiling fwd, dx, dw;
+  bool rows_kernel;                                  // few rows: the forward product and dx have a kernel of their own
 };
 struct LinearPlan {
-  size_t status, x_parts, w_parts, dz, dz_parts, db_part, dw_part, fwd_total, total;
+  size_t status, x_parts, w_parts, dz, dz_parts, db_part, sums, total;
 };
 
-int resolve(const switch_moe_linear_config* cfg, LinearShape* s) {
+int resolve(const switch_moe_linear_config* cfg, bool backward, LinearShape* s) {
   if (cfg == nullptr) return SWITCH_MOE_INVALID_ARGUMENT;
   const switch_moe_linear_config& c = *cfg;
   if (c.M < 0 || c.K <= 0 || c.N <= 0 || c.ldx < 0 || c.ldw < 0 || c.ldy < 0 || c.reserved[0] != 0 || c.reserved[1] != 0)
@@ -52,23 +53,29 @@ int resolve(const switch_moe_linear_config* cfg, LinearShape* s) {
   s->chunk_rows = (int)rows;
   s->chunks = (int)(((long long)c.M + rows - 1) / rows);
   if (s->chunks > 65535 || col_blocks > 0x7fffffffll) return SWITCH_MOE_UNSUPPORTED_SHAPE;
-  s->dw_splits = dense_splits(c.K, c.N, c.M);
+  s->rows_kernel = few_rows(s->f32, c.M);
+  const DenseTiling none{1, 256};
+  s->fwd = backward || s->rows_kernel ? none : dense_tiling(kDenseFwd, s->f32, c.M, c.N, c.K);
+  s->dx = !backward || s->rows_kernel ? none : dense_tiling(kDenseDx, s->f32, c.M, c.K, c.N);
+  s->dw = !backward ? none : dense_tiling(kDenseDw, s->f32, c.K, c.N, c.M);
   return SWITCH_MOE_OK;
 }
 
-void make_plan(const LinearShape& s, LinearPlan* p) {
+// The forward and the backward call lay the workspace out each for itself.
+void make_plan(const LinearShape& s, bool backward, LinearPlan* p) {
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off = (off + bytes + 1023) / 1024 * 1024; return o; };
+  auto part_bytes = [](const DenseTiling& g, size_t rows, size_t ld) { return g.splits > 1 ? g.splits * rows * ld * 4 : 0; };
   const size_t M = s.M, K = s.K;
+  const bool own_dz = backward && (s.act != SWITCH_MOE_ACT_NONE || s.q > 0), parts = s.f32;
   p->status = take(kStatusWords * 4);
-  p->x_parts = take(s.f32 ? 3 * M * s.ldk * 2 : 0);
-  p->w_parts = take(s.f32 ? 3 * K * s.ldn * 2 : 0);
-  p->fwd_total = off;
-  const bool own_dz = s.act != SWITCH_MOE_ACT_NONE || s.q > 0;
+  p->x_parts = take(parts && (backward || !s.rows_kernel) ? 3 * M * s.ldk * 2 : 0);
+  p->w_parts = take(parts && !s.rows_kernel ? 3 * K * s.ldn * 2 : 0);
   p->dz = take(own_dz ? M * s.ldn * s.elt : 0);
-  p->dz_parts = take(s.f32 ? 3 * M * s.ldn * 2 : 0);
-  p->db_part = take((size_t)s.chunks * s.ldn * 4);
-  p->dw_part = take(s.dw_splits > 1 ? (size_t)s.dw_splits * K * s.ldn * 4 : 0);
+  p->dz_parts = take(backward && parts ? 3 * M * s.ldn * 2 : 0);
+  p->db_part = take(backward ? (size_t)s.chunks * s.ldn * 4 : 0);
+  const size_t fwd = part_bytes(s.fwd, M, s.ldn), dx = part_bytes(s.dx, M, s.ldk), dw = part_bytes(s.dw, K, s.ldn);
+  p->sums = take(fwd + (dx > dw ? dx : dw));           // (fwd, or dx and then dw)
   p->total = off;
 }
 
@@ -264,26 +271,28 @@ linear_parts_kernel(const float* __restrict__ src, long long ld, long long rows,
   }
 }
 
-// out = sum of the parts, in order.
+// The sum of a split contraction's parts, in order, and what comes after the product.
 template <typename ET>
 __global__ void __launch_bounds__(kThreads)
-linear_add_kernel(const float* __restrict__ part, int splits, long long rows, int cols, long long ld_part, ET* out, long long ld_out) {
+linear_add_kernel(const float* __restrict__ part, int splits, long long rows, int cols, long long ld_part, DenseEpilogue e,
+                  void* out, long long ld_out) {
   pdl_launch_dependents();
   pdl_wait();
+  const DropoutState rng = dropout_state(e.dropout);
   const long long per_row = ld_part / 8, total = rows * per_row;
   for (long long b = (long long)blockIdx.x * kThreads + threadIdx.x; b < total; b += (long long)gridDim.x * kThreads) {
-    const long long row = b / per_row;
+    const long long row = total <= 0x7fffffffll ? (long long)((unsigned)b / (unsigned)per_row) : b / per_row;
     const int col = (int)(b - row * per_row) * 8;
-    const int n = cols - col < 8 ? cols - col : 8;
     float s[8];
-    load8(part + row * ld_part + col, n, s);
+    load8(part + row * ld_part + col, 8, s);          // (the parts' rows are whole eights; what is beyond cols is not stored)
+#pragma unroll 4
     for (int i = 1; i < splits; ++i) {
       float f[8];
-      load8(part + ((long long)i * rows + row) * ld_part + col, n, f);
+      load8(part + ((long long)i * rows + row) * ld_part + col, 8, f);
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[j] += f[j];
     }
-    store8(out + row * ld_out + col, n, s);
+    finish8<ET>(e, rng, out, ld_out, cols, row, col, s);
   }
 }
 
@@ -295,6 +304,20 @@ unsigned flat_grid(long long threads) {
 int launch_parts(const void* src, long long ld, long long rows, int cols, long long ld_out, __nv_bfloat16* parts, cudaStream_t st) {
   launch_k(linear_parts_kernel, dim3(flat_grid(rows * (ld_out / 8))), dim3(kThreads), 0, st, static_cast<const float*>(src), ld,
            rows, cols, ld_out, parts);
+  return launch_status();
+}
+
+// One product, split or not; `out` and `ld_out` are the result's.
+int launch_product(DenseKind kind, DenseProduct q, const DenseTiling& g, const DenseEpilogue& e, float* sums, long long ld_sums,
+                   void* out, long long ld_out, cudaStream_t st) {
+  q.splits = g.splits; q.width = g.width;
+  q.out = g.splits > 1 ? sums : out;
+  q.ld_out = g.splits > 1 ? ld_sums : ld_out;
+  const int rc = launch_dense(kind, q, g.splits > 1 ? DenseEpilogue{} : e, st);
+  if (rc != SWITCH_MOE_OK || g.splits == 1) return rc;
+  const dim3 grid(flat_grid((long long)q.rows * (ld_sums / 8)));
+  launch_k(q.f32 ? linear_add_kernel<float> : linear_add_kernel<__nv_bfloat16>, grid, dim3(kThreads), 0, st,
+           static_cast<const float*>(sums), g.splits, (long long)q.rows, q.cols, ld_sums, e, out, ld_out);
   return launch_status();
 }
 
@@ -333,11 +356,15 @@ using namespace swmoe;
 
 extern "C" int switch_moe_linear_workspace_bytes(const switch_moe_linear_config* cfg, int32_t backward, size_t* bytes_out) {
   if (bytes_out == nullptr) return SWITCH_MOE_INVALID_ARGUMENT;
-  LinearShape s;
-  SWMOE_TRY(resolve(cfg, &s));
-  LinearPlan p;
-  make_plan(s, &p);
-  *bytes_out = backward != 0 ? p.total : p.fwd_total;
+  size_t most = 0;
+  for (int pass = 0; pass <= (backward != 0 ? 1 : 0); ++pass) {
+    LinearShape s;
+    SWMOE_TRY(resolve(cfg, pass == 1, &s));
+    LinearPlan p;
+    make_plan(s, pass == 1, &p);
+    if (p.total > most) most = p.total;
+  }
+  *bytes_out = most;
   return SWITCH_MOE_OK;
 }
 
@@ -345,10 +372,10 @@ extern "C" int switch_moe_linear_fwd(const switch_moe_linear_config* cfg, const 
                                      const void* residual, const uint64_t* rng, void* y, void* pre, void* workspace,
                                      size_t workspace_bytes, void* stream) {
   LinearShape s;
-  SWMOE_TRY(resolve(cfg, &s));
+  SWMOE_TRY(resolve(cfg, false, &s));
   LinearPlan p;
-  make_plan(s, &p);
-  SWMOE_TRY(check_workspace(workspace, workspace_bytes, p.fwd_total));
+  make_plan(s, false, &p);
+  SWMOE_TRY(check_workspace(workspace, workspace_bytes, p.total));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   int* status = ws_ptr<int>(workspace, p.status);
   if (s.M == 0)
@@ -358,12 +385,12 @@ extern "C" int switch_moe_linear_fwd(const switch_moe_linear_config* cfg, const 
       (reinterpret_cast<uintptr_t>(rng) & 7u) != 0)
     return SWITCH_MOE_UNSUPPORTED_SHAPE;
   DenseProduct q{};
-  q.rows = s.M; q.cols = s.N; q.k = s.K; q.f32 = s.f32; q.splits = 1;
+  q.rows = s.M; q.cols = s.N; q.k = s.K; q.f32 = s.f32;
   q.a = {x, s.ldx, static_cast<const float*>(x), s.ldx, 1};
   q.b = {W, s.ldw, static_cast<const float*>(W), 1, s.ldw};
   q.out = y; q.ld_out = s.ldy; q.status = status; q.clear_status = true;
   const DenseEpilogue e{bias, residual, pre, s.act, (int)(s.ldn / 8), dropout_params(rng, s.q, s.site)};
-  if (few_rows(s.f32, s.M)) return launch_dense_rows(kDenseFwd, q, e, st);
+  if (s.rows_kernel) return launch_dense_rows(kDenseFwd, q, e, st);
   if (s.f32) {
     __nv_bfloat16* xp = ws_ptr<__nv_bfloat16>(workspace, p.x_parts);
     __nv_bfloat16* wp = ws_ptr<__nv_bfloat16>(workspace, p.w_parts);
@@ -372,16 +399,16 @@ extern "C" int switch_moe_linear_fwd(const switch_moe_linear_config* cfg, const 
     q.a.p = xp; q.a.ld = s.ldk;
     q.b.p = wp; q.b.ld = s.ldn;
   }
-  return launch_dense(kDenseFwd, q, e, st);
+  return launch_product(kDenseFwd, q, s.fwd, e, ws_ptr<float>(workspace, p.sums), s.ldn, y, s.ldy, st);
 }
 
 extern "C" int switch_moe_linear_bwd(const switch_moe_linear_config* cfg, const void* dy, const void* x, const void* W,
                                      const void* pre, const uint64_t* rng, void* workspace, size_t workspace_bytes,
                                      void* dx, void* dW, float* dbias, void* stream) {
   LinearShape s;
-  SWMOE_TRY(resolve(cfg, &s));
+  SWMOE_TRY(resolve(cfg, true, &s));
   LinearPlan p;
-  make_plan(s, &p);
+  make_plan(s, true, &p);
   SWMOE_TRY(check_workspace(workspace, workspace_bytes, p.total));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (!aligned16(dy) || !aligned16(x) || !aligned16(W) || !aligned16(pre) || !aligned16(dx) || !aligned16(dW) ||
@@ -417,11 +444,11 @@ extern "C" int switch_moe_linear_bwd(const switch_moe_linear_config* cfg, const 
   DenseOperand go{s.f32 ? dz_parts : g, s.f32 ? s.ldn : ldg, static_cast<const float*>(g), 0, 0};
   if (dx != nullptr) {
     DenseProduct q{};
-    q.rows = s.M; q.cols = s.K; q.k = s.N; q.f32 = s.f32; q.splits = 1;
+    q.rows = s.M; q.cols = s.K; q.k = s.N; q.f32 = s.f32;
     q.a = go; q.a.si = ldg; q.a.sk = 1;
     q.b = {W, s.ldw, static_cast<const float*>(W), s.ldw, 1};
     q.out = dx; q.ld_out = s.ldx; q.status = status; q.clear_status = !cleared;
-    if (few_rows(s.f32, s.M)) {
+    if (s.rows_kernel) {
       q.a.p = g; q.a.ld = ldg;
       SWMOE_TRY(launch_dense_rows(kDenseDx, q, DenseEpilogue{}, st));
     } else {
@@ -430,13 +457,13 @@ extern "C" int switch_moe_linear_bwd(const switch_moe_linear_config* cfg, const 
         SWMOE_TRY(launch_parts(W, s.ldw, s.K, s.N, s.ldn, wp, st));
         q.b.p = wp; q.b.ld = s.ldn;
       }
-      SWMOE_TRY(launch_dense(kDenseDx, q, DenseEpilogue{}, st));
+      SWMOE_TRY(launch_product(kDenseDx, q, s.dx, DenseEpilogue{}, ws_ptr<float>(workspace, p.sums), s.ldk, dx, s.ldx, st));
     }
     cleared = true;
   }
   if (dW != nullptr) {
     DenseProduct q{};
-    q.rows = s.K; q.cols = s.N; q.k = s.M; q.f32 = s.f32; q.splits = s.dw_splits;
+    q.rows = s.K; q.cols = s.N; q.k = s.M; q.f32 = s.f32;
     q.a = {x, s.ldx, static_cast<const float*>(x), 1, s.ldx};
     q.b = go; q.b.si = 1; q.b.sk = ldg;
     if (s.f32) {
@@ -445,21 +472,7 @@ extern "C" int switch_moe_linear_bwd(const switch_moe_linear_config* cfg, const 
       q.a.p = xp; q.a.ld = s.ldk;
     }
     q.status = status; q.clear_status = !cleared;
-    float* part = ws_ptr<float>(workspace, p.dw_part);
-    q.out = s.dw_splits > 1 ? part : dW;
-    q.ld_out = s.dw_splits > 1 ? s.ldn : s.ldw;
-    SWMOE_TRY(launch_dense(kDenseDw, q, DenseEpilogue{}, st));
-    if (s.dw_splits > 1) {
-      const dim3 grid(flat_grid((long long)s.K * (s.ldn / 8)));
-      const float* cp = part;
-      if (s.f32)
-        launch_k(linear_add_kernel<float>, grid, dim3(kThreads), 0, st, cp, s.dw_splits, (long long)s.K, s.N, s.ldn,
-                 static_cast<float*>(dW), s.ldw);
-      else
-        launch_k(linear_add_kernel<__nv_bfloat16>, grid, dim3(kThreads), 0, st, cp, s.dw_splits, (long long)s.K, s.N, s.ldn,
-                 static_cast<__nv_bfloat16*>(dW), s.ldw);
-      SWMOE_TRY(launch_status());
-    }
+    SWMOE_TRY(launch_product(kDenseDw, q, s.dw, DenseEpilogue{}, ws_ptr<float>(workspace, p.sums), s.ldn, dW, s.ldw, st));
   }
   return SWITCH_MOE_OK;
 }
@@ -467,7 +480,7 @@ extern "C" int switch_moe_linear_bwd(const switch_moe_linear_config* cfg, const 
 extern "C" int switch_moe_linear_check_device_status(const switch_moe_linear_config* cfg, void* workspace,
                                                      int32_t* info_out, void* stream) {
   LinearShape s;
-  SWMOE_TRY(resolve(cfg, &s));
+  SWMOE_TRY(resolve(cfg, false, &s));
   SWMOE_TRY(check_workspace(workspace, ~(size_t)0, 0));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   int32_t host[kStatusWords];

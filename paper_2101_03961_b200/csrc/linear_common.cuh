@@ -30,7 +30,7 @@ struct DenseEpilogue {    // forward pass only
 struct DenseProduct {
   int rows, cols, k;
   int f32;                // operands as parts, float32 result
-  int splits;             // > 1: `out` is float32 [splits][rows][ld_out], to be added up
+  int splits, width;      // dense_tiling's choice; splits > 1: `out` is float32 [splits][rows][ld_out], to be added up
   DenseOperand a, b;
   void* out;
   long long ld_out;
@@ -43,7 +43,11 @@ enum DenseKind { kDenseFwd = 0, kDenseDx = 1, kDenseDw = 2 };   // A, B k-major:
 // Forward product and dx of few rows: a kernel of their own (linear_rows.cu).
 inline bool few_rows(bool f32, long long rows) { return rows <= (f32 ? 16 : 64); }
 int launch_dense_rows(DenseKind kind, const DenseProduct& q, const DenseEpilogue& e, cudaStream_t st);
-int dense_splits(long long rows, long long cols, long long k);
+// Into how many parts the contraction is cut, and the columns of a tile.
+struct DenseTiling {
+  int splits, width;
+};
+DenseTiling dense_tiling(DenseKind kind, bool f32, long long rows, long long cols, long long k);
 int launch_dense(DenseKind kind, const DenseProduct& q, const DenseEpilogue& e, cudaStream_t st);
 
 // The float32 operands of the tensor cores: x 2^24 as the exact sum of three bfloat16 values (f32_gemm_sm100.cu).
@@ -123,6 +127,59 @@ __device__ __forceinline__ float2 gelu_grad_pair(float z0, float z1) {
   // 1/2 + e (poly + a / sqrt(2 pi))
   const float2 h = halves_of(pair_fma(e, pair_fma(a, pair_same(0.3989422804014327f), poly), pair_same(0.5f)));
   return halves_of(pair_add(pair_of(copysignf(h.x, z0), copysignf(h.y, z1)), pair_same(0.5f)));
+}
+
+// Everything after the product for eight results of a row: bias, z saved, activation, dropout, residual, store.
+template <typename ET>
+__device__ __forceinline__ void finish8(const DenseEpilogue& e, const DropoutState& rng, void* out, long long ld, int cols,
+                                        long long row, int col, float* x) {
+  const int n = min(8, cols - col);
+  const long long at = row * ld + col;
+  auto put = [&](void* base, const float* v) {
+    ET* o = static_cast<ET*>(base) + at;
+    if constexpr (sizeof(ET) == 2) {
+      if (n == 8) {
+        __nv_bfloat162 h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        *reinterpret_cast<uint4*>(o) = *reinterpret_cast<const uint4*>(h);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < n) o[i] = __float2bfloat16(v[i]);
+      }
+    } else {
+      if (n == 8) {
+        *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
+        *reinterpret_cast<float4*>(o + 4) = make_float4(v[4], v[5], v[6], v[7]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < n) o[i] = v[i];
+      }
+    }
+  };
+  if (e.bias != nullptr) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] += i < n ? e.bias[col + i] : 0.f;
+  }
+  if (e.pre != nullptr) put(e.pre, x);
+  if (e.activation == SWITCH_MOE_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = max_nan(x[i], 0.f);
+  } else if (e.activation == SWITCH_MOE_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) gelu_pair(x + i, x + i + 1);
+  }
+  if (e.dropout.rng != nullptr)
+    dropout8(e.dropout, dropout_bits(e.dropout, rng, (unsigned long long)row * (unsigned)e.dropout_blocks + (unsigned)(col >> 3)), x);
+  if (e.residual != nullptr) {
+    const ET* r = static_cast<const ET*>(e.residual) + at;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) x[i] += (float)r[i];
+  }
+  put(out, x);
 }
 
 }  // namespace swmoe

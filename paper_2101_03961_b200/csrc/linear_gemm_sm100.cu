@@ -18,6 +18,7 @@
 // and sums from 2^80 on end there too).
 //
 // Every wait is bounded in time; after one gave up all roles leave.
+#include <algorithm>
 #include <cmath>
 #include <type_traits>
 
@@ -153,7 +154,7 @@ __device__ __forceinline__ Unit decode(const DenseParams& p, int id, int TN) {
 template <bool kAMn, bool kBMn, int TN, int kMode>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant__ DenseParams p) {
-  constexpr bool kFwd = !kAMn && kBMn;                       // the only product with an epilogue of its own
+  constexpr bool kFwd = !kAMn && kBMn && kMode != kPartial;  // the only product with an epilogue of its own
   constexpr bool kOut4 = kMode != kBf16;                     // float32 output
   // This CTA's half of B: TN / 2 columns x 64 steps (n-major in boxes of 64 columns, of which TN = 192 uses one and a half)
   constexpr int kBBoxes = (TN / 2 + 63) / 64, kBBytes = kBMn ? kBBoxes * kAtomBytes : TN * 64;
@@ -327,8 +328,8 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
     // step over all of them, not column after column: a store to shared memory between two columns would keep the second
     // one's loads behind it, and the warps (four a scheduler) wait for their own results often enough.
     auto finish = [&](auto count, float* x, const float* bias, long long row, int col, auto&& saved) {
-      constexpr int C = decltype(count)::value;
       if constexpr (kFwd) {
+        constexpr int C = decltype(count)::value;
         if (p.bias != nullptr) {
 #pragma unroll
           for (int i = 0; i < C; i += 4) {
@@ -618,27 +619,9 @@ int launch_kernel(const DenseMaps& m, const DenseParams& p, cudaStream_t st) {
   return launch_status();
 }
 
-// Tile width: the one whose rounds over the CTA pairs cost least.  A narrower tile costs more than its share, since A is
-// staged as before: measured 0.86 (0.80 where B is k-major and no box of it is wasted) and 0.62 of a 256-wide tile's time for
-// 192 and 128 columns.  us with 256 / 192 / 128 columns: 32768 tokens, 768 x 2048 forward 82 / 101 / 115, dx 87 / 81 / 94; 8192
-// tokens dx 25 / 21 / 23; 4100, 768 x 520 forward 11.1 / 10.9 / 10.4; 1000, 768 x 2048 10.2 / 9.6 / 8.1.  Float32, where a part
-// staged once serves two or three products: 0.75 and 0.5 (4001, 512 x 2048 forward 51 / 58 / 50, dx 84 / 72 / 56).
-int tile_columns(long long rows, long long cols, long long splits, bool k_major, bool f32) {
-  const long long pairs = kChipSms / 2, m = (rows + 255) / 256;
-  const double share[3] = {1.0, f32 ? 0.75 : k_major ? 0.80 : 0.86, f32 ? 0.51 : 0.62};
-  int best = 256;
-  double best_cost = 0;
-  for (int i = 0; i < 3; ++i) {
-    const int w = 256 - 64 * i;
-    const double cost = (double)((m * ((cols + w - 1) / w) * splits + pairs - 1) / pairs) * share[i];
-    if (best_cost == 0 || cost < best_cost) { best = w; best_cost = cost; }
-  }
-  return best;
-}
-
 template <bool kAMn, bool kBMn, int kMode>
 int launch_kind(const DenseProduct& q, const DenseEpilogue& e, cudaStream_t st) {
-  const int TN = tile_columns(q.rows, q.cols, q.splits, !kBMn, q.f32);
+  const int TN = q.width;
   DenseParams p{};
   p.rows = q.rows; p.cols = q.cols; p.k = q.k;
   p.k_blocks = (int)(((long long)q.k + kBK - 1) / kBK);
@@ -672,29 +655,42 @@ int launch_kind(const DenseProduct& q, const DenseEpilogue& e, cudaStream_t st) 
 
 }  // namespace
 
-// Into how many parts the contraction is cut: where the output has too few tiles for the pairs, as in a weight gradient,
-// so that the last round of units is full; at least 16 blocks of 64 steps a part, whose sums are written and read once more.
-int dense_splits(long long rows, long long cols, long long k) {
-  const long long pairs = kChipSms / 2, tiles = ((rows + 255) / 256) * ((cols + 255) / 256), blocks = (k + kBK - 1) / kBK;
-  int best = 1;
-  double best_cost = 0;
-  for (int s = 1; s <= 16; ++s) {
+// The tiling whose estimated time is least.  A round of tiles over the CTA pairs takes a time per 64 steps of the contraction
+// that falls with the width, but by less than the width does, since A is staged as before (us with 256 / 192 / 128 columns:
+// 32768 tokens, 2048 x 768 forward 78 / 82 / 88, dx of 768 x 2048, k-major, 87 / 81 / 94; 8192 tokens, 768 x 2048 22.4 / 24.2 /
+// 25.3; 1000 tokens 10.2 / 9.6 / 8.1; float32 4001, 512 x 2048 forward 51 / 58 / 50, dx 84 / 72 / 56), and one for its
+// epilogue.  Cutting the contraction fills the pairs where the output has few tiles, a weight gradient's or that of a few
+// hundred tokens; the parts are written and read once more, by one more launch.
+DenseTiling dense_tiling(DenseKind kind, bool f32, long long rows, long long cols, long long k) {
+  const long long pairs = kChipSms / 2, m = (rows + 255) / 256, blocks = (k + kBK - 1) / kBK;
+  const double step_us[3] = {f32 ? 3.0 : 0.40, f32 ? 2.25 : kind == kDenseDx ? 0.32 : 0.35, f32 ? 1.5 : 0.25};
+  const double round_us = f32 ? 3.0 : 1.0, join_us = 3.5, part_us = (double)rows * (double)cols * 8.0 / 4e6;   // 4 TB/s
+  DenseTiling best{1, 256};
+  double best_us = 0;
+  // (twice as many units as pairs at most, and coarser steps as parts get many: this runs in every call)
+  const long long most = std::min(32ll, 2 * pairs / (m * ((cols + 255) / 256)));
+  for (int s = 1; s == 1 || s <= most; s += s < 8 ? 1 : s < 16 ? 2 : 8) {
     const long long per = (blocks + s - 1) / s;
-    if (s > 1 && (per < 16 || (s - 1) * per >= blocks)) continue;
-    const long long rounds = (tiles * s + pairs - 1) / pairs;
-    // in blocks of a 256 x 256 tile, 0.3 us each: the products, and 256 KB a tile and part written and read at 6 TB/s by all pairs
-    const double cost = (double)rounds * (double)per + (s > 1 ? 8.0 + 0.3 * (double)(tiles * s) : 0.0);
-    if (best_cost == 0 || cost < best_cost) { best = s; best_cost = cost; }
+    if (s > 1 && (per < 4 || (s - 1) * per >= blocks)) continue;      // (no part without work)
+    for (int i = 0; i < 3; ++i) {
+      const int w = 256 - 64 * i;
+      const long long rounds = (m * ((cols + w - 1) / w) * s + pairs - 1) / pairs;
+      const double us = (double)rounds * ((double)per * step_us[i] + round_us) + (s > 1 ? join_us + s * part_us : 0.0);
+      if (best_us == 0 || us < best_us) { best = {s, w}; best_us = us; }
+    }
   }
   return best;
 }
 
+template <bool kAMn, bool kBMn>
+int launch_mode(const DenseProduct& q, const DenseEpilogue& e, cudaStream_t st) {
+  if (q.f32) return launch_kind<kAMn, kBMn, kF32>(q, e, st);
+  return q.splits > 1 ? launch_kind<kAMn, kBMn, kPartial>(q, e, st) : launch_kind<kAMn, kBMn, kBf16>(q, e, st);
+}
+
 int launch_dense(DenseKind kind, const DenseProduct& q, const DenseEpilogue& e, cudaStream_t st) {
-  const int mode = q.f32 ? kF32 : q.splits > 1 ? kPartial : kBf16;
-  if (kind == kDenseFwd) return mode == kF32 ? launch_kind<false, true, kF32>(q, e, st) : launch_kind<false, true, kBf16>(q, e, st);
-  if (kind == kDenseDx) return mode == kF32 ? launch_kind<false, false, kF32>(q, e, st) : launch_kind<false, false, kBf16>(q, e, st);
-  return mode == kF32 ? launch_kind<true, true, kF32>(q, e, st)
-                      : mode == kPartial ? launch_kind<true, true, kPartial>(q, e, st) : launch_kind<true, true, kBf16>(q, e, st);
+  if (kind == kDenseFwd) return launch_mode<false, true>(q, e, st);
+  return kind == kDenseDx ? launch_mode<false, false>(q, e, st) : launch_mode<true, true>(q, e, st);
 }
 
 }  // namespace swmoe

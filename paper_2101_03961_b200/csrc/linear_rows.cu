@@ -56,60 +56,6 @@ __device__ __forceinline__ float4 remote4(uint32_t local, uint32_t cta) {
   return v;
 }
 
-// Eight results of a row: everything after the product.
-template <typename ET>
-__device__ __forceinline__ void finish8(const RowsParams& p, const DropoutState& rng, long long row, int col, float* x) {
-  const int n = min(8, p.N - col);
-  const long long at = row * p.ld_out + col;
-  auto put = [&](void* base, const float* v) {
-    ET* o = static_cast<ET*>(base) + at;
-    if constexpr (sizeof(ET) == 2) {
-      if (n == 8) {
-        __nv_bfloat162 h[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-        *reinterpret_cast<uint4*>(o) = *reinterpret_cast<const uint4*>(h);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i < n) o[i] = __float2bfloat16(v[i]);
-      }
-    } else {
-      if (n == 8) {
-        *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
-        *reinterpret_cast<float4*>(o + 4) = make_float4(v[4], v[5], v[6], v[7]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i < n) o[i] = v[i];
-      }
-    }
-  };
-  if (p.e.bias != nullptr) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] += i < n ? p.e.bias[col + i] : 0.f;
-  }
-  if (p.e.pre != nullptr) put(p.e.pre, x);
-  if (p.e.activation == SWITCH_MOE_ACT_RELU) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = x[i] < 0.f ? 0.f : x[i];
-  } else if (p.e.activation == SWITCH_MOE_ACT_GELU) {
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) gelu_pair(x + i, x + i + 1);
-  }
-  if (p.e.dropout.rng != nullptr) {
-    const uint4 bits = dropout_bits(p.e.dropout, rng, (unsigned long long)row * (unsigned)p.e.dropout_blocks + (unsigned)(col >> 3));
-        dropout8(p.e.dropout, bits, x);
-  }
-  if (p.e.residual != nullptr) {
-    const ET* r = static_cast<const ET*>(p.e.residual) + at;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) x[i] += (float)r[i];
-  }
-  put(p.out, x);
-}
-
 // What this thread's first eight results need from memory, on its way to L2 while the weights come in.
 template <typename ET>
 __device__ __forceinline__ void prefetch_epilogue(const RowsParams& p, int rank, int col0) {
@@ -138,7 +84,7 @@ __device__ __forceinline__ void join_slices(const RowsParams& p, const float* su
       x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w;
       x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
     }
-    finish8<ET>(p, rng, row, col, x);
+    finish8<ET>(p.e, rng, p.out, p.ld_out, p.N, row, col, x);
   }
   if (p.slices > 1) cluster_sync();                   // no block leaves while another still reads its sums
 }
