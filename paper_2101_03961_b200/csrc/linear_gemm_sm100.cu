@@ -20,7 +20,6 @@
 // Every wait is bounded in time; after one gave up all roles leave.
 #include <algorithm>
 #include <cmath>
-#include <type_traits>
 
 #include "linear_common.cuh"
 #include "tc_common.cuh"
@@ -324,36 +323,33 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
     if (kFwd) rng = dropout_state(p.dropout);
     uint32_t it = 0, n_block = 0, res_phase = 0;             // res_phase: a bit per buffer
     bool ok = true;
-    // Bias, then (once `saved` has been called with z) activation and dropout of C columns of this thread's row.  Step after
+    // Bias, then (once `saved` has been called with z) activation and dropout of 32 columns of this thread's row.  Step after
     // step over all of them, not column after column: a store to shared memory between two columns would keep the second
     // one's loads behind it, and the warps (four a scheduler) wait for their own results often enough.
-    auto finish = [&](auto count, float* x, const float* bias, long long row, int col, auto&& saved) {
+    auto finish = [&](float* x, long long row, int col, auto&& saved) {
       if constexpr (kFwd) {
-        constexpr int C = decltype(count)::value;
         if (p.bias != nullptr) {
 #pragma unroll
-          for (int i = 0; i < C; i += 4) {
-            const float4 b = *reinterpret_cast<const float4*>(bias + i);
+          for (int i = 0; i < 32; i += 4) {
+            const float4 b = *reinterpret_cast<const float4*>(bias_w + i);
             x[i] += b.x; x[i + 1] += b.y; x[i + 2] += b.z; x[i + 3] += b.w;
           }
         }
         if (pre) saved(x);
         if (p.activation == SWITCH_MOE_ACT_RELU) {
 #pragma unroll
-          for (int i = 0; i < C; ++i) x[i] = max_nan(x[i], 0.f);
+          for (int i = 0; i < 32; ++i) x[i] = max_nan(x[i], 0.f);
         } else if (p.activation == SWITCH_MOE_ACT_GELU) {
 #pragma unroll
-          for (int i = 0; i < C; i += 2) gelu_pair(x + i, x + i + 1);
+          for (int i = 0; i < 32; i += 2) gelu_pair(x + i, x + i + 1);
         }
         if (p.dropout.rng != nullptr) {
           const unsigned long long block = (unsigned long long)row * (unsigned)p.dropout_blocks + (unsigned)(col >> 3);
 #pragma unroll
-          for (int i = 0; i < C / 8; ++i) dropout8(p.dropout, dropout_bits(p.dropout, rng, block + i), x + 8 * i);
+          for (int i = 0; i < 4; ++i) dropout8(p.dropout, dropout_bits(p.dropout, rng, block + i), x + 8 * i);
         }
       }
     };
-    using eight = std::integral_constant<int, 8>;
-    using all32 = std::integral_constant<int, 32>;
     // Of a tile's blocks of 32 columns this warp has every fourth: one or two.
     constexpr int kMost = (TN / 32 + 3) / 4;
     const int n_blocks = TN == 192 ? (quarter < 2 ? 2 : 1) : kMost;
@@ -424,11 +420,14 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
         const uint32_t buf = pre || kOut4 ? 0u : (n_block & 1u) * kBufferBytes;
         uint32_t v[32];
         if constexpr (kMode != kF32) tc_ld32(taddr0 + (it & 1u) * 256u + 128u * b, v);
+        auto buffers_read = [&] {                            // this block's (and with `ahead` the next one's) buffers have
+          if (pre || kOut4 || ahead) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");   // been read by their
+          else asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");                         // last stores
+        };
         if (inside) {
-          if (lane == 0) {                                   // this block's (and the next one's) buffers have been read by
-            if (pre || kOut4 || ahead) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");   // their last stores
-            else asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-            if (residual && !ahead && !kOut4) fetch_residual(buf, col0, row0);
+          if (residual && !kOut4 && lane == 0) {             // (else: when the accumulator is there, below)
+            buffers_read();
+            if (!ahead) fetch_residual(buf, col0, row0);
           }
           if (ahead) fetch_after(id, b + 1, buf ^ kBufferBytes);
           if (kFwd && p.bias != nullptr) bias_w[lane] = b == 0 ? bias_r[0] : bias_r[kMost - 1];
@@ -443,6 +442,10 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
           }
         }
         if (!inside) continue;
+        if (!residual || kOut4) {
+          if (lane == 0) buffers_read();
+          __syncwarp();
+        }
         if (residual && !kOut4) {
           const uint32_t bit = buf ? 2u : 1u;
           ok = mbar_wait_warp(res_bar + (buf ? 8u : 0u), (res_phase & bit) ? 1u : 0u, abort_flag, p.status, 45);
@@ -453,87 +456,95 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
         auto piece_at = [&](int j) -> float4* {              // float32: 16-byte piece j (0 .. 7) of the row's 32 columns
           return reinterpret_cast<float4*>(stage_g + (j >> 2) * kBufferBytes + row_off + (((uint32_t)(j & 3) ^ sw) << 4));
         };
+        const bool edge = col0 + 32 > p.whole_cols && row < p.rows;     // columns that belong to no whole 16 bytes
+        float x[32];
         if constexpr (kMode == kF32) {
-          // The sums go through the staging buffers, so that the loop over them need not be unrolled.
-          auto dump = [&](const float* s) {
+          bool finite = true;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) *piece_at(j) = make_float4(s[4 * j], s[4 * j + 1], s[4 * j + 2], s[4 * j + 3]);
-          };
-          if (kMost == 1 || b == 0) dump(sum);
-          else dump(sum + (kMost == 1 ? 0 : 32));
+          for (int i = 0; i < 32; ++i) {
+            x[i] = (kMost == 1 || b == 0 ? sum[i] : sum[kMost == 1 ? 0 : 32 + i]) * kPartDown;
+            finite = finite && isfinite(x[i]);
+          }
+          if (!finite && row < p.rows) {                     // formed again, by way of this thread's row of the buffers
+#pragma unroll
+            for (int j = 0; j < 8; ++j) *piece_at(j) = make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
+            const float* pa = p.a + row * p.a_si;
+            const long long k1 = min(p.k, (long long)u.kb1 * kBK);
 #pragma unroll 1
-          for (int j = 0; j < 4; ++j) {
-            const int col = col0 + 8 * j;
-            if (col >= p.cols || row >= p.rows) break;
-            const float4 lo = *piece_at(2 * j), hi = *piece_at(2 * j + 1);
-            float x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-            bool finite = true;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              x[i] *= kPartDown;
-              finite = finite && isfinite(x[i]);
+            for (int i = 0; i < 32 && col0 + i < p.cols; ++i) {
+              float* at = reinterpret_cast<float*>(piece_at(i >> 2)) + (i & 3);
+              if (isfinite(*at)) continue;
+              float again = 0.f;
+              const float* pb = p.b + (long long)(col0 + i) * p.b_si;
+              for (long long k = (long long)u.kb0 * kBK; k < k1; ++k) again = fmaf(pa[k * p.a_sk], pb[k * p.b_sk], again);
+              *at = again;
+              for (uint32_t cta = 0; cta < 2; ++cta)         // the waiting warps of both CTAs see that work goes on
+                store_at(progress, cta, (uint32_t)clock64());
             }
-            if (!finite) {
-#pragma unroll 1
-              for (int i = 0; i < 8; ++i) {
-                if (col + i >= p.cols) break;
-                float again = 0.f;
-                const float* pa = p.a + row * p.a_si;
-                const float* pb = p.b + (long long)(col + i) * p.b_si;
-                const long long k1 = min(p.k, (long long)u.kb1 * kBK);
-                for (long long k = (long long)u.kb0 * kBK; k < k1; ++k) again = fmaf(pa[k * p.a_sk], pb[k * p.b_sk], again);
 #pragma unroll
-                for (int n = 0; n < 8; ++n)
-                  if (n == i && !isfinite(x[n])) x[n] = again;
-                for (uint32_t cta = 0; cta < 2; ++cta)       // the waiting warps of both CTAs see that work goes on
-                  store_at(progress, cta, (uint32_t)clock64());
-              }
+            for (int j = 0; j < 8; ++j) {
+              const float4 f = *piece_at(j);
+              x[4 * j] = f.x; x[4 * j + 1] = f.y; x[4 * j + 2] = f.z; x[4 * j + 3] = f.w;
             }
-            const long long at = row * p.ld_out + col;
-            const bool whole = col + 8 <= p.whole_cols;
-            finish(eight{}, x, bias_w + 8 * j, row, col, [&](const float* z) {
-              float* o = static_cast<float*>(p.pre) + at;
-              if (whole) {
-                *reinterpret_cast<float4*>(o) = make_float4(z[0], z[1], z[2], z[3]);
-                *reinterpret_cast<float4*>(o + 4) = make_float4(z[4], z[5], z[6], z[7]);
-              } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                  if (col + i < p.cols) o[i] = z[i];
-              }
-            });
-            if (residual) {
-              const float* rs = static_cast<const float*>(p.residual) + at;
-#pragma unroll
-              for (int i = 0; i < 8; ++i)
-                if (col + i < p.cols) x[i] += rs[i];
-            }
-            if (!whole) store_ragged<true>(p, p.out, u.split * p.split_out + at, col, x);
-            *piece_at(2 * j) = make_float4(x[0], x[1], x[2], x[3]);
-            *piece_at(2 * j + 1) = make_float4(x[4], x[5], x[6], x[7]);
           }
           __syncwarp();
         } else {
-          const bool edge = col0 + 32 > p.whole_cols && row < p.rows;   // columns that belong to no whole 16 bytes
-          float x[32];
 #pragma unroll
           for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(v[i]);
-          auto at16 = [&](uint8_t* row_at, int j) { return reinterpret_cast<uint4*>(row_at + (((uint32_t)j ^ sw) << 4)); };
-          auto put = [&](uint8_t* row_at, const float* f) {  // bf16: the row's four pieces of 16 bytes
+        }
+        auto at16 = [&](uint8_t* row_at, int j) { return reinterpret_cast<uint4*>(row_at + (((uint32_t)j ^ sw) << 4)); };
+        auto put = [&](uint8_t* row_at, const float* f) {    // bf16: four pieces of 16 bytes; float32: eight, in both buffers
+          if constexpr (kOut4) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) *piece_at(j) = make_float4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
+          } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
               *at16(row_at, j) = make_uint4(pack2_bf16(f[8 * j], f[8 * j + 1]), pack2_bf16(f[8 * j + 2], f[8 * j + 3]),
                                             pack2_bf16(f[8 * j + 4], f[8 * j + 5]), pack2_bf16(f[8 * j + 6], f[8 * j + 7]));
-          };
-          auto put_edge = [&](void* to, long long at, const float* f) {
+          }
+        };
+        auto put_edge = [&](void* to, long long at, const float* f) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) store_ragged<kOut4>(p, to, at + 8 * j, col0 + 8 * j, f + 8 * j);
-          };
-          finish(all32{}, x, bias_w, row, col0, [&](const float* z) {
-            if (edge) put_edge(p.pre, row * p.ld_out + col0, z);
-            put(stage_g + kBufferBytes + row_off, z);
-          });
-          if (residual) {
+          for (int j = 0; j < 4; ++j) store_ragged<kOut4>(p, to, at + 8 * j, col0 + 8 * j, f + 8 * j);
+        };
+        auto send4 = [&](const CUtensorMap* map, int split) {           // float32: both buffers
+          if (col0 < p.whole_cols) store_box(map, stage_s, col0, row0, split);
+          if (col0 + 16 < p.whole_cols) store_box(map, stage_s + kBufferBytes, col0 + 16, row0, split);
+        };
+        finish(x, row, col0, [&](const float* z) {
+          if (edge) put_edge(p.pre, row * p.ld_out + col0, z);
+          put(stage_g + kBufferBytes + row_off, z);
+          if constexpr (kOut4) {                             // on its way before the results take its place
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+              send4(&maps.pre, 0);
+              asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            }
+          }
+        });
+        if (kOut4 && pre) {
+          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+          __syncwarp();
+        }
+        if (residual) {
+          if constexpr (kOut4) {
+            const float* rs = static_cast<const float*>(p.residual) + row * p.ld_out + col0;
+            if (row < p.rows) {
+#pragma unroll
+              for (int i = 0; i < 32; i += 4) {
+                if (col0 + i + 4 <= p.cols) {
+                  const float4 f = *reinterpret_cast<const float4*>(rs + i);
+                  x[i] += f.x; x[i + 1] += f.y; x[i + 2] += f.z; x[i + 3] += f.w;
+                } else {
+#pragma unroll
+                  for (int n = 0; n < 4; ++n)
+                    if (col0 + i + n < p.cols) x[i + n] += rs[i + n];
+                }
+              }
+            }
+          } else {
             uint4 q[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) q[j] = *at16(dst, j);
@@ -547,20 +558,18 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
               }
             }
           }
-          if (edge) put_edge(p.out, u.split * p.split_out + row * p.ld_out + col0, x);
-          if constexpr (kOut4) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) *piece_at(j) = make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
-          } else {
-            put(dst, x);
-          }
         }
+        if (edge) put_edge(p.out, u.split * p.split_out + row * p.ld_out + col0, x);
+        put(dst, x);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) {
-          if (col0 < p.whole_cols) store_box(&maps.out, stage_s + buf, col0, row0, u.split);
-          if (kOut4 && col0 + 16 < p.whole_cols) store_box(&maps.out, stage_s + kBufferBytes, col0 + 16, row0, u.split);
-          if (pre && !kOut4 && col0 < p.whole_cols) store_box(&maps.pre, stage_s + kBufferBytes, col0, row0, 0);
+          if constexpr (kOut4) {
+            send4(&maps.out, u.split);
+          } else if (col0 < p.whole_cols) {
+            store_box(&maps.out, stage_s + buf, col0, row0, u.split);
+            if (pre) store_box(&maps.pre, stage_s + kBufferBytes, col0, row0, 0);
+          }
           asm volatile("cp.async.bulk.commit_group;" ::: "memory");
         }
         ++n_block;
