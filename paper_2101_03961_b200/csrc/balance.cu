@@ -22,6 +22,7 @@ constexpr int kFinalExperts = 32;                    // experts per block of the
 
 struct BalanceShape {
   int T, E, k, G, Tg, blocks;      // blocks per group
+  bool alone;                      // one block does everything
   long long ld;
   float alpha;
   int f32;
@@ -49,6 +50,7 @@ int resolve(const switch_moe_balance_config* cfg, BalanceShape* s) {
   long long want = ((long long)4 * kChipSms + G - 1) / G, most = (s->Tg + 8 * kWarps - 1) / (8 * kWarps);
   s->blocks = (int)(want < most ? want : most);
   if (s->blocks < 1) s->blocks = 1;
+  s->alone = false;                // (decided where the layout is known)
   return SWITCH_MOE_OK;
 }
 
@@ -97,6 +99,24 @@ template <> struct Piece<float, 1> {
 template <> struct Piece<__nv_bfloat16, 1> {
   static __device__ __forceinline__ void load(const __nv_bfloat16* p, float* f) { *f = __bfloat162float(*p); }
   static __device__ __forceinline__ void store(__nv_bfloat16* p, const float* f) { *p = __float2bfloat16(*f); }
+};
+
+// float32 pairs and bfloat16 pairs and fours: rows that are not 16-byte aligned, but whose parts are
+template <> struct Piece<float, 2> {
+  static __device__ __forceinline__ void load(const float* p, float* f) {
+    const float2 v = *reinterpret_cast<const float2*>(p);
+    f[0] = v.x; f[1] = v.y;
+  }
+  static __device__ __forceinline__ void store(float* p, const float* f) { *reinterpret_cast<float2*>(p) = make_float2(f[0], f[1]); }
+};
+template <> struct Piece<__nv_bfloat16, 2> {
+  static __device__ __forceinline__ void load(const __nv_bfloat16* p, float* f) {
+    const float2 v = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(p));
+    f[0] = v.x; f[1] = v.y;
+  }
+  static __device__ __forceinline__ void store(__nv_bfloat16* p, const float* f) {
+    *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(f[0], f[1]);
+  }
 };
 
 template <typename T>
@@ -164,7 +184,7 @@ struct Row {
 template <typename ET, int V, int NV>
 __global__ void __launch_bounds__(kThreads)
 balance_rows_kernel(const ET* logits, const int* index, const uint8_t* mask, BalanceShape s, int L, unsigned* ticket,
-                    int* tokens_out, int* counts_out, float* psum_out) {
+                    int* tokens_out, int* counts_out, float* psum_out, float* loss) {
   pdl_launch_dependents();
   pdl_wait();
   extern __shared__ int smem[];                       // counts [E], then sums [warps][E]
@@ -263,17 +283,29 @@ balance_rows_kernel(const ET* logits, const int* index, const uint8_t* mask, Bal
   if (lane == 0) warp_tokens[warp] = n;
   __syncthreads();
   const long long part = (long long)g * gridDim.x + blockIdx.x;
+  double term = 0.0;
   for (int e = threadIdx.x; e < s.E; e += kThreads) {
     float p = 0.f;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) p += sums[w * s.E + e];
-    psum_out[part * s.E + e] = p;
     counts_out[part * s.E + e] = smem[e];
+    if (!s.alone) psum_out[part * s.E + e] = p;
+    else term += (double)smem[e] * (double)p;
   }
+  int total = 0;
+  for (int w = 0; w < kWarps; ++w) total += warp_tokens[w];
+  if (threadIdx.x == 0) tokens_out[part] = total;
+  if (!s.alone) return;
+  // the only block: counts and tokens went to the caller's arrays, and the loss follows from its own sums
+  __shared__ double terms[kWarps];
+  for (int o = 16; o > 0; o >>= 1) term += __shfl_xor_sync(0xffffffffu, term, o);
+  if (lane == 0) terms[warp] = term;
+  __syncthreads();
   if (threadIdx.x == 0) {
-    int total = 0;
-    for (int w = 0; w < kWarps; ++w) total += warp_tokens[w];
-    tokens_out[part] = total;
+    term = 0.0;
+    for (int w = 0; w < kWarps; ++w) term += terms[w];
+    const double n2 = total > 0 ? (double)total * total : 1.0;
+    *loss = total > 0 ? (float)((double)s.alpha * s.E * term / (s.k * n2)) : 0.f;
   }
 }
 
@@ -384,46 +416,47 @@ balance_bwd_kernel(const ET* logits, const uint8_t* mask, const int* counts, con
   }
 }
 
-// Calls f with the row layout of a shape: pieces of 16 bytes where every row starts on one, else single elements.
+// Calls f with the row layout of a shape: pieces of the most bytes, up to 16, on whose multiples every row starts and ends.
 template <typename ET, typename F>
-int with_layout(const BalanceShape& s, bool vector, F&& f) {
+int with_layout(const BalanceShape& s, const void* a, const void* b, F&& f) {
   constexpr int W = 16 / (int)sizeof(ET);
-  const int V = vector ? W : 1;
+  const uintptr_t at = reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b) | (uintptr_t)(s.ld * sizeof(ET)) |
+                       (uintptr_t)(s.E * sizeof(ET));
+  const int V = at % 16 == 0 ? W : at % (2 * sizeof(ET)) == 0 ? 2 : 1;
   const int pieces = (s.E + V - 1) / V;
-  // Few lanes a row, 16 elements each, so that the rows of a warp share the steps of its reductions; but four lanes at
-  // least (64 consecutive bytes), and with single elements as many as there are.
+  // Few lanes a row, 16 elements each (8 in small pieces), so that the rows of a warp share the steps of its reductions; but
+  // at least 64 consecutive bytes.
   int L = 1;
-  while (L < 32 && L < pieces && (V == 1 || L < 4 || pieces * V > 16 * L)) L *= 2;
+  while (L < 32 && L < pieces && (L * V * (int)sizeof(ET) < 64 || pieces * V > (V == W ? 16 : 8) * L)) L *= 2;
   const int nv = (pieces + L - 1) / L;
   using std::integral_constant;
 #define SWMOE_NV(vv, n) \
   if (V == vv && nv <= n) return f(integral_constant<int, vv>{}, integral_constant<int, n>{}, L);
   SWMOE_NV(W, 1) SWMOE_NV(W, 2) SWMOE_NV(W, 4)
   if constexpr (W == 4) { SWMOE_NV(W, 8) }
-  SWMOE_NV(1, 1) SWMOE_NV(1, 2) SWMOE_NV(1, 4) SWMOE_NV(1, 8) SWMOE_NV(1, 16) SWMOE_NV(1, 32)
+  SWMOE_NV(2, 1) SWMOE_NV(2, 2) SWMOE_NV(2, 4) SWMOE_NV(2, 16)
+  SWMOE_NV(1, 1) SWMOE_NV(1, 2) SWMOE_NV(1, 4) SWMOE_NV(1, 8) SWMOE_NV(1, 32)
 #undef SWMOE_NV
   return SWITCH_MOE_UNSUPPORTED_SHAPE;
 }
 
 template <typename ET>
-bool vector_rows(const BalanceShape& s, const void* a, const void* b) {
-  return s.E * sizeof(ET) % 16 == 0 && s.ld * sizeof(ET) % 16 == 0 && aligned16(a) && aligned16(b);
-}
-
-template <typename ET>
-int forward(const BalanceShape& s, const BalancePlan& p, const void* logits, const int32_t* index, const uint8_t* mask,
+int forward(BalanceShape s, const BalancePlan& p, const void* logits, const int32_t* index, const uint8_t* mask,
             float* loss, int32_t* counts, int32_t* tokens, void* ws, cudaStream_t st) {
   unsigned* ticket = ws_ptr<unsigned>(ws, p.ticket);
   int* tp = ws_ptr<int>(ws, p.tokens);
   int* cp = ws_ptr<int>(ws, p.counts);
   float* pp = ws_ptr<float>(ws, p.psum);
-  const int rc = with_layout<ET>(s, vector_rows<ET>(s, logits, logits), [&](auto v, auto nv, int L) {
+  const int rc = with_layout<ET>(s, logits, logits, [&](auto v, auto nv, int L) {
     const size_t smem = (size_t)s.E * 4 * (1 + kWarps);
+    // What one block does in four steps of its warps is one block and one launch: the second one takes 2.5 us of host time.
+    s.alone = s.G == 1 && s.T <= 4 * kWarps * (32 / L);
+    if (s.alone) { s.blocks = 1; tp = tokens; cp = counts; }
     launch_k(balance_rows_kernel<ET, decltype(v)::value, decltype(nv)::value>, dim3(s.blocks, s.G), dim3(kThreads), smem, st,
-             static_cast<const ET*>(logits), index, mask, s, L, ticket, tp, cp, pp);
+             static_cast<const ET*>(logits), index, mask, s, L, ticket, tp, cp, pp, loss);
     return launch_status();
   });
-  if (rc != SWITCH_MOE_OK) return rc;
+  if (rc != SWITCH_MOE_OK || s.alone) return rc;
   launch_k(balance_sum_kernel, dim3((s.E + kFinalExperts - 1) / kFinalExperts, s.G), dim3(kThreads), 0, st,
            static_cast<const int*>(tp), static_cast<const int*>(cp), static_cast<const float*>(pp), s, ticket,
            ws_ptr<float>(ws, p.loss_part), loss, counts, tokens);
@@ -434,7 +467,7 @@ template <typename ET>
 int backward(const BalanceShape& s, const void* logits, const uint8_t* mask, const int32_t* counts, const int32_t* tokens,
              float d_loss, void* dlogits, cudaStream_t st) {
   const float factor = (float)((double)d_loss * s.alpha * s.E / ((double)s.k * s.G));
-  return with_layout<ET>(s, vector_rows<ET>(s, logits, dlogits), [&](auto v, auto nv, int L) {
+  return with_layout<ET>(s, logits, dlogits, [&](auto v, auto nv, int L) {
     const int rows_per_block = kWarps * (32 / L);
     long long most = ((long long)s.Tg + rows_per_block - 1) / rows_per_block;
     const long long want = ((long long)16 * kChipSms + s.G - 1) / s.G;

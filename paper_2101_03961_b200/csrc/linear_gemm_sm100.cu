@@ -677,7 +677,7 @@ DenseTiling dense_tiling(DenseKind kind, bool f32, long long rows, long long col
   DenseTiling best{1, 256};
   double best_us = 0;
   // (twice as many units as pairs at most, and coarser steps as parts get many: this runs in every call)
-  const long long most = std::min(32ll, 2 * pairs / (m * ((cols + 255) / 256)));
+  const long long most = std::min(std::min(32ll, blocks / 4), 2 * pairs / (m * ((cols + 255) / 256)));
   for (int s = 1; s == 1 || s <= most; s += s < 8 ? 1 : s < 16 ? 2 : 8) {
     const long long per = (blocks + s - 1) / s;
     if (s > 1 && (per < 4 || (s - 1) * per >= blocks)) continue;      // (no part without work)

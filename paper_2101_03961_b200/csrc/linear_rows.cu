@@ -2,8 +2,9 @@
 // bfloat16 or 16 of float32.  Such a call reads W once and little else, so it is all latency and bandwidth: a tile of the
 // tensor-core kernel (256 rows, one CTA pair per 128 columns and all of the contraction) would leave most SMs without work.
 //
-// Here a block has 64 output columns and a slice of the contraction; the blocks of the other slices form a cluster with it
-// and add their sums up through distributed shared memory, in rank order.  64-deep pieces of W and x come in by cp.async,
+// Here a block has 64 output columns and a slice of the contraction; the blocks of the other slices form a cluster with it.
+// The rows x 8 groups of eight outputs are dealt out to the cluster's blocks; each block writes its sums into the shared memory
+// of the one that finishes them, and after one cluster barrier that one adds them up in a fixed order.  64-deep pieces of W and x come in by cp.async,
 // up to kStages at a time.  bfloat16: warp-level MMAs (16 columns of W x 8 rows of x x 16 steps: with so few rows a
 // tcgen05 tile would be padding, and the loads bound it in either case); float32: fused multiply-adds.
 // One token, 768 x 2048, GELU: 3.1 MB of weights.
@@ -15,7 +16,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kCols = 64, kDepth = 64;               // output columns of a block; steps per stage
 constexpr int kMaxSlices = 8;
-constexpr int kPad = kCols + 4;                      // floats between rows of the sums
 
 struct RowsParams {
   const void* x; const void* W;
@@ -45,48 +45,55 @@ __device__ __forceinline__ void mma16816(float* d, const uint32_t* a, uint32_t b
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void push(uint32_t local, uint32_t cta, float v) {
+  asm volatile("{\n\t.reg .b32 ra;\n\tmapa.shared::cluster.u32 ra, %0, %1;\n\tst.shared::cluster.f32 [ra], %2;\n\t}" ::"r"(local),
+               "r"(cta), "f"(v) : "memory");
 }
-__device__ __forceinline__ float4 remote4(uint32_t local, uint32_t cta) {
-  float4 v;
-  asm volatile("{\n\t.reg .b32 ra;\n\tmapa.shared::cluster.u32 ra, %4, %5;\n\t"
-               "ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [ra];\n\t}"
-               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(local), "r"(cta) : "memory");
-  return v;
-}
+
+// Where a block keeps what the others push: [source][group of its own][8], a source being a slice and a part of a block's steps.
+struct Sums {
+  uint32_t base;
+  int groups, slices;                                 // groups of eight per block
+  __device__ __forceinline__ Sums(const RowsParams& p, uint32_t at) : base(at), groups((8 * p.M + p.slices - 1) / p.slices), slices(p.slices) {}
+  // group g of the 8 M (row g / 8, columns 8 (g % 8) ..) belongs to block g % slices
+  __device__ __forceinline__ void put(int source, int g, int i, float v) const {
+    const int own = g / slices;
+    push(base + (uint32_t)(((source * groups + own) * 8 + i) * 4), (uint32_t)(g - own * slices), v);
+  }
+};
 
 // What this thread's first eight results need from memory, on its way to L2 while the weights come in.
 template <typename ET>
 __device__ __forceinline__ void prefetch_epilogue(const RowsParams& p, int rank, int col0) {
-  const int u = rank * kThreads + threadIdx.x, row = u >> 3, col = col0 + (u & 7) * 8;
+  const int g = threadIdx.x * p.slices + rank, row = g >> 3, col = col0 + (g & 7) * 8;
   if (row >= p.M || col >= p.N) return;
   if (p.e.bias != nullptr) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.e.bias + col));
   if (p.e.residual != nullptr)
     asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const ET*>(p.e.residual) + row * p.ld_out + col));
 }
 
-// The sums of this block lie in `sums` [M][kPad]; the cluster's blocks share the rows x 8 groups of eight columns out.
+// After the pushes: the groups of this block.  `sources` per slice.
 template <typename ET>
-__device__ __forceinline__ void join_slices(const RowsParams& p, const float* sums, int rank, int col0) {
+__device__ __forceinline__ void join_slices(const RowsParams& p, const float* sums, int sources, int rank, int col0) {
   const DropoutState rng = dropout_state(p.e.dropout);
-  const uint32_t base = smem_at(sums);
-  if (p.slices > 1) cluster_sync();
-  else __syncthreads();
-  for (int u = rank * kThreads + threadIdx.x; u < 8 * p.M; u += p.slices * kThreads) {
-    const int row = u >> 3, col = col0 + (u & 7) * 8;
-    if (col >= p.N) continue;
+  cluster_arrive();
+  cluster_wait();
+  const int groups = (8 * p.M + p.slices - 1) / p.slices;
+  for (int own = threadIdx.x; own < groups; own += kThreads) {
+    const int g = own * p.slices + rank, row = g >> 3, col = col0 + (g & 7) * 8;
+    if (row >= p.M || col >= p.N) continue;
     float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const uint32_t at = base + (uint32_t)(row * kPad + (u & 7) * 8) * 4u;
 #pragma unroll 4
-    for (int s = 0; s < p.slices; ++s) {
-      const float4 a = remote4(at, s), b = remote4(at + 16u, s);
+    for (int s = 0; s < sources * p.slices; ++s) {
+      const float4 a = *reinterpret_cast<const float4*>(sums + (s * groups + own) * 8);
+      const float4 b = *reinterpret_cast<const float4*>(sums + (s * groups + own) * 8 + 4);
       x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w;
       x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
     }
     finish8<ET>(p.e, rng, p.out, p.ld_out, p.N, row, col, x);
   }
-  if (p.slices > 1) cluster_sync();                   // no block leaves while another still reads its sums
 }
 
 // kNK: W is stored [output column][contraction] (dx), else [contraction][output column].  NT: tiles of eight rows of x.
@@ -103,6 +110,7 @@ linear_rows_kernel(const RowsParams p) {
   const int total = (int)((p.K + kDepth - 1) / kDepth), count = max(0, min(p.depth_per_slice, total - first));
   const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(p.x);
   const __nv_bfloat16* W = static_cast<const __nv_bfloat16*>(p.W);
+  cluster_arrive();
   pdl_wait();
   if (p.status != nullptr && blockIdx.x == 0 && threadIdx.x < kStatusWords) p.status[threadIdx.x] = 0;
   // Tiles have rows of 128 bytes, their 16-byte pieces exchanged by the row.
@@ -172,24 +180,16 @@ linear_rows_kernel(const RowsParams p) {
       }
     }
   }
-  asm volatile("cp.async.wait_group 0;" ::: "memory");
-  __syncthreads();                                    // the stages' memory is free: the sums go there
-  float* sums = reinterpret_cast<float*>(smem);
-  const int c = 16 * cg + (lane >> 2), r = 2 * (lane & 3);
+  const Sums sums(p, smem_at(smem) + kStages * kStage);
+  cluster_wait();                                     // every block of the cluster is there to be written to
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {                       // the halves of the steps, one after the other
-    if (kh == h) {
+  for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float* at = sums + (8 * t + r + (i & 1)) * kPad + c + 8 * (i >> 1);
-          *at = h == 0 ? acc[t][i] : *at + acc[t][i];
-        }
+    for (int i = 0; i < 4; ++i) {
+      const int row = 8 * t + 2 * (lane & 3) + (i & 1), group = 2 * cg + (i >> 1);
+      if (row < p.M) sums.put(2 * rank + kh, 8 * row + group, lane >> 2, acc[t][i]);
     }
-    __syncthreads();
-  }
-  join_slices<__nv_bfloat16>(p, sums, rank, col0);
+  join_slices<__nv_bfloat16>(p, reinterpret_cast<const float*>(smem + kStages * kStage), 2, rank, col0);
 }
 
 // float32: thread = one column x a quarter of a stage's steps, MT rows in registers.
@@ -205,6 +205,7 @@ linear_rows_f32_kernel(const RowsParams p) {
   const int total = (int)((p.K + kDepth - 1) / kDepth), count = max(0, min(p.depth_per_slice, total - first));
   const float* x = static_cast<const float*>(p.x);
   const float* W = static_cast<const float*>(p.W);
+  cluster_arrive();
   pdl_wait();
   if (p.status != nullptr && blockIdx.x == 0 && threadIdx.x < kStatusWords) p.status[threadIdx.x] = 0;
   // W's tile has rows of 256 bytes, their 16-byte pieces exchanged by the row where lanes read down a column of pieces.
@@ -265,18 +266,12 @@ linear_rows_f32_kernel(const RowsParams p) {
       }
     }
   }
-  asm volatile("cp.async.wait_group 0;" ::: "memory");
-  __syncthreads();
-  float* sums = reinterpret_cast<float*>(smem);
+  const Sums sums(p, smem_at(smem) + kStages * kStage);
+  cluster_wait();
 #pragma unroll
-  for (int h = 0; h < 4; ++h) {
-    if (kq == h) {
-#pragma unroll
-      for (int m = 0; m < MT; ++m) sums[m * kPad + c] = h == 0 ? acc[m] : sums[m * kPad + c] + acc[m];
-    }
-    __syncthreads();
-  }
-  join_slices<float>(p, sums, rank, col0);
+  for (int m = 0; m < MT; ++m)
+    if (m < p.M) sums.put(4 * rank + kq, 8 * m + (c >> 3), c & 7, acc[m]);
+  join_slices<float>(p, reinterpret_cast<const float*>(smem + kStages * kStage), 4, rank, col0);
 }
 
 template <typename Kern>
@@ -307,12 +302,15 @@ int launch(Kern kernel, size_t smem, int slices, const RowsParams& p, bool* read
 template <bool kNK, int NT>
 int launch_bf16(const RowsParams& p, cudaStream_t st) {
   static bool ready[64] = {false};
-  return launch(linear_rows_kernel<kNK, NT>, (size_t)6 * (kCols * kDepth * 2 + NT * 8 * kDepth * 2), p.slices, p, ready, st);
+  // stages, then two sums a slice for every output (the groups per block rounded up)
+  return launch(linear_rows_kernel<kNK, NT>, (size_t)6 * (kCols * kDepth * 2 + NT * 8 * kDepth * 2) + 2 * (NT * 8 * 8 + kMaxSlices) * 32,
+                p.slices, p, ready, st);
 }
 template <bool kNK, int MT>
 int launch_f32(const RowsParams& p, cudaStream_t st) {
   static bool ready[64] = {false};
-  return launch(linear_rows_f32_kernel<kNK, MT>, (size_t)4 * (kCols * kDepth * 4 + MT * kDepth * 4), p.slices, p, ready, st);
+  return launch(linear_rows_f32_kernel<kNK, MT>, (size_t)4 * (kCols * kDepth * 4 + MT * kDepth * 4) + 4 * (MT * 8 + kMaxSlices) * 32,
+                p.slices, p, ready, st);
 }
 template <bool kNK>
 int launch_any(const DenseProduct& q, const RowsParams& p, cudaStream_t st) {

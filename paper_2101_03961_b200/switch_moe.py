@@ -354,11 +354,11 @@ def _refuse(where: str, name: str, why: str):
 
 # A call's host time is most of a small call's time, so a check that passes is a few attribute reads (0.5 us a tensor); what
 # did not fit is worked out only to be reported.
-def _matrix(where, name, t, dtype, rows, cols, ld):
+def _matrix(where, dev, name, t, dtype, rows, cols, ld):
     """Pointer of a [rows, cols] tensor with `ld` elements between rows (0: cols), or of None."""
     if t is None or t.__class__ is int:
         return t
-    if t.dtype is dtype and t.shape == (rows, cols) and t.get_device() == _current_device():
+    if t.dtype is dtype and t.shape == (rows, cols) and t.get_device() == dev:
         s = t.stride()
         if (s[0] == (ld or cols) or rows <= 1) and (s[1] == 1 or cols == 1):
             return t.data_ptr()
@@ -370,11 +370,11 @@ def _matrix(where, name, t, dtype, rows, cols, ld):
     _refuse(where, name, f"has strides {t.stride()}, not {(ld or cols, 1)}")
 
 
-def _vector(where, name, t, dtypes, n):
+def _vector(where, dev, name, t, dtypes, n):
     """Pointer of a contiguous tensor of n elements, or of None."""
     if t is None or t.__class__ is int:
         return t
-    if t.dtype in dtypes and t.numel() == n and t.is_contiguous() and t.get_device() == _current_device():
+    if t.dtype in dtypes and t.numel() == n and t.is_contiguous() and t.get_device() == dev:
         return t.data_ptr()
     if t.dtype not in dtypes:
         _refuse(where, name, f"is {t.dtype}")
@@ -383,10 +383,10 @@ def _vector(where, name, t, dtypes, n):
     _check_device(where, name, t)
 
 
-def _workspace_args(where, t):
+def _workspace_args(where, dev, t):
     if t is None:
         return None, 0
-    if t.is_contiguous() and t.get_device() == _current_device():
+    if t.is_contiguous() and t.get_device() == dev:
         return t.data_ptr(), t.nbytes
     _check_device(where, "workspace", t)
     _refuse(where, "workspace", "is not contiguous")
@@ -439,21 +439,21 @@ def allocate_balance_workspace(cfg: BalanceConfig, device="cuda") -> torch.Tenso
 def switch_moe_linear_fwd(cfg, x, W, bias, residual, rng, y, pre, workspace, stream=None) -> None:
     """x [M, K], W [K, N], bias float32 [N] or None, residual [M, N] or None, rng int64 [2] {key, offset} (None without
     dropout); writes y [M, N] and, unless it is None, pre [M, N]."""
-    f, M, K, N, ldy, dt = "switch_moe_linear_fwd", cfg.M, cfg.K, cfg.N, cfg.ldy, _TORCH_TYPES.get(cfg.dtype)
+    f, dev, M, K, N, ldy, dt = "switch_moe_linear_fwd", _current_device(), cfg.M, cfg.K, cfg.N, cfg.ldy, _TORCH_TYPES.get(cfg.dtype)
     _check((_lib or load_library()).switch_moe_linear_fwd(
-        cfg, _matrix(f, "x", x, dt, M, K, cfg.ldx), _matrix(f, "W", W, dt, K, N, cfg.ldw), _vector(f, "bias", bias, _FLOAT, N),
-        _matrix(f, "residual", residual, dt, M, N, ldy), _vector(f, "rng", rng, _RNG_TYPES, 2), _matrix(f, "y", y, dt, M, N, ldy),
-        _matrix(f, "pre", pre, dt, M, N, ldy), *_workspace_args(f, workspace), _stream(stream)), f)
+        cfg, _matrix(f, dev, "x", x, dt, M, K, cfg.ldx), _matrix(f, dev, "W", W, dt, K, N, cfg.ldw), _vector(f, dev, "bias", bias, _FLOAT, N),
+        _matrix(f, dev, "residual", residual, dt, M, N, ldy), _vector(f, dev, "rng", rng, _RNG_TYPES, 2), _matrix(f, dev, "y", y, dt, M, N, ldy),
+        _matrix(f, dev, "pre", pre, dt, M, N, ldy), *_workspace_args(f, dev, workspace), _stream(stream)), f)
 
 
 def switch_moe_linear_bwd(cfg, dy, x, W, pre, rng, workspace, dx, dW, dbias, stream=None) -> None:
     """Writes dx [M, K], dW [K, N], dbias float32 [N]; each may be None.  The residual's gradient is dy."""
-    f, M, K, N, ldx, ldw, ldy = "switch_moe_linear_bwd", cfg.M, cfg.K, cfg.N, cfg.ldx, cfg.ldw, cfg.ldy
+    f, dev, M, K, N, ldx, ldw, ldy = "switch_moe_linear_bwd", _current_device(), cfg.M, cfg.K, cfg.N, cfg.ldx, cfg.ldw, cfg.ldy
     dt = _TORCH_TYPES.get(cfg.dtype)
     _check((_lib or load_library()).switch_moe_linear_bwd(
-        cfg, _matrix(f, "dy", dy, dt, M, N, ldy), _matrix(f, "x", x, dt, M, K, ldx), _matrix(f, "W", W, dt, K, N, ldw),
-        _matrix(f, "pre", pre, dt, M, N, ldy), _vector(f, "rng", rng, _RNG_TYPES, 2), *_workspace_args(f, workspace),
-        _matrix(f, "dx", dx, dt, M, K, ldx), _matrix(f, "dW", dW, dt, K, N, ldw), _vector(f, "dbias", dbias, _FLOAT, N),
+        cfg, _matrix(f, dev, "dy", dy, dt, M, N, ldy), _matrix(f, dev, "x", x, dt, M, K, ldx), _matrix(f, dev, "W", W, dt, K, N, ldw),
+        _matrix(f, dev, "pre", pre, dt, M, N, ldy), _vector(f, dev, "rng", rng, _RNG_TYPES, 2), *_workspace_args(f, dev, workspace),
+        _matrix(f, dev, "dx", dx, dt, M, K, ldx), _matrix(f, dev, "dW", dW, dt, K, N, ldw), _vector(f, dev, "dbias", dbias, _FLOAT, N),
         _stream(stream)), f)
 
 
@@ -468,35 +468,35 @@ def switch_moe_linear_check_device_status(cfg, workspace, stream=None) -> list:
 
 def switch_moe_dropout_fwd(cfg, x, residual, rng, y, stream=None) -> None:
     """y = residual + dropout(x); residual may be None, y may be x or residual."""
-    f, rows, cols, ld, dt = "switch_moe_dropout_fwd", cfg.rows, cfg.cols, cfg.ld, _TORCH_TYPES.get(cfg.dtype)
+    f, dev, rows, cols, ld, dt = "switch_moe_dropout_fwd", _current_device(), cfg.rows, cfg.cols, cfg.ld, _TORCH_TYPES.get(cfg.dtype)
     _check((_lib or load_library()).switch_moe_dropout_fwd(
-        cfg, _matrix(f, "x", x, dt, rows, cols, ld), _matrix(f, "residual", residual, dt, rows, cols, ld),
-        _vector(f, "rng", rng, _RNG_TYPES, 2), _matrix(f, "y", y, dt, rows, cols, ld), _stream(stream)), f)
+        cfg, _matrix(f, dev, "x", x, dt, rows, cols, ld), _matrix(f, dev, "residual", residual, dt, rows, cols, ld),
+        _vector(f, dev, "rng", rng, _RNG_TYPES, 2), _matrix(f, dev, "y", y, dt, rows, cols, ld), _stream(stream)), f)
 
 
 def switch_moe_dropout_bwd(cfg, dy, rng, dx, stream=None) -> None:
     """dx = dropout(dy) with the mask of the forward call; dx may be dy."""
-    f, rows, cols, ld, dt = "switch_moe_dropout_bwd", cfg.rows, cfg.cols, cfg.ld, _TORCH_TYPES.get(cfg.dtype)
+    f, dev, rows, cols, ld, dt = "switch_moe_dropout_bwd", _current_device(), cfg.rows, cfg.cols, cfg.ld, _TORCH_TYPES.get(cfg.dtype)
     _check((_lib or load_library()).switch_moe_dropout_bwd(
-        cfg, _matrix(f, "dy", dy, dt, rows, cols, ld), _vector(f, "rng", rng, _RNG_TYPES, 2),
-        _matrix(f, "dx", dx, dt, rows, cols, ld), _stream(stream)), f)
+        cfg, _matrix(f, dev, "dy", dy, dt, rows, cols, ld), _vector(f, dev, "rng", rng, _RNG_TYPES, 2),
+        _matrix(f, dev, "dx", dx, dt, rows, cols, ld), _stream(stream)), f)
 
 
 def switch_moe_balance_fwd(cfg, logits, expert_index, token_mask, loss, counts, tokens, workspace, stream=None) -> None:
     """logits [T, E]; expert_index int32 [T, k] or None (the k largest logits); token_mask uint8 or bool [T] or None; writes
     loss float32 [1], counts int32 [groups, E], tokens int32 [groups]."""
-    f, T, E, G = "switch_moe_balance_fwd", cfg.T, cfg.E, cfg.groups or 1
+    f, dev, T, E, G = "switch_moe_balance_fwd", _current_device(), cfg.T, cfg.E, cfg.groups or 1
     _check((_lib or load_library()).switch_moe_balance_fwd(
-        cfg, _matrix(f, "logits", logits, _TORCH_TYPES.get(cfg.dtype), T, E, cfg.ld),
-        _vector(f, "expert_index", expert_index, _INT, T * cfg.k), _vector(f, "token_mask", token_mask, _MASK_TYPES, T),
-        _vector(f, "loss", loss, _FLOAT, 1), _vector(f, "counts", counts, _INT, G * E), _vector(f, "tokens", tokens, _INT, G),
-        *_workspace_args(f, workspace), _stream(stream)), f)
+        cfg, _matrix(f, dev, "logits", logits, _TORCH_TYPES.get(cfg.dtype), T, E, cfg.ld),
+        _vector(f, dev, "expert_index", expert_index, _INT, T * cfg.k), _vector(f, dev, "token_mask", token_mask, _MASK_TYPES, T),
+        _vector(f, dev, "loss", loss, _FLOAT, 1), _vector(f, dev, "counts", counts, _INT, G * E), _vector(f, dev, "tokens", tokens, _INT, G),
+        *_workspace_args(f, dev, workspace), _stream(stream)), f)
 
 
 def switch_moe_balance_bwd(cfg, logits, token_mask, counts, tokens, d_loss, dlogits, stream=None) -> None:
     """dlogits [T, E] from the counts and tokens of the forward call; dlogits may be logits."""
-    f, T, E, G, ld, dt = "switch_moe_balance_bwd", cfg.T, cfg.E, cfg.groups or 1, cfg.ld, _TORCH_TYPES.get(cfg.dtype)
+    f, dev, T, E, G, ld, dt = "switch_moe_balance_bwd", _current_device(), cfg.T, cfg.E, cfg.groups or 1, cfg.ld, _TORCH_TYPES.get(cfg.dtype)
     _check((_lib or load_library()).switch_moe_balance_bwd(
-        cfg, _matrix(f, "logits", logits, dt, T, E, ld), _vector(f, "token_mask", token_mask, _MASK_TYPES, T),
-        _vector(f, "counts", counts, _INT, G * E), _vector(f, "tokens", tokens, _INT, G), float(d_loss),
-        _matrix(f, "dlogits", dlogits, dt, T, E, ld), _stream(stream)), f)
+        cfg, _matrix(f, dev, "logits", logits, dt, T, E, ld), _vector(f, dev, "token_mask", token_mask, _MASK_TYPES, T),
+        _vector(f, dev, "counts", counts, _INT, G * E), _vector(f, dev, "tokens", tokens, _INT, G), float(d_loss),
+        _matrix(f, dev, "dlogits", dlogits, dt, T, E, ld), _stream(stream)), f)
