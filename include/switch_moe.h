@@ -304,7 +304,7 @@ int switch_moe_stage_launches(const switch_moe_config* cfg, int32_t* launches_ou
  * conventions above hold (device pointers, one stream, status codes, gradients overwritten), with two differences:
  * tensors are rows at a stated distance (ld.. fields, 0 = dense; a distance in bytes is a multiple of 16, and what lies
  * between a row's end and the next row is neither read nor written), and the arithmetic is float32 or wider with one
- * rounding of each result to the tensor's type.
+ * rounding of each result to the tensor's type.  No dimension may exceed 2^30 (UNSUPPORTED_SHAPE).
  *
  * Dropout.  The mask is a function of the element's place and a state, and is never stored: forward and backward
  * compute it where they need it.  `rng` is DEVICE uint64[2], read when the kernel runs, so that a captured graph draws
@@ -339,7 +339,8 @@ int switch_moe_linear_workspace_bytes(const switch_moe_linear_config* cfg, int32
 /* Forward.  x [M,K]; W [K,N]; bias float32[N] or NULL; residual [M,N] or NULL (may be y itself); rng: see above;
  * y [M,N] (out); pre [M,N] (out) receives z for the backward pass, or NULL.  x, W and bias may not overlap y or pre.
  * bf16: products on the tensor cores, float32 sums; f32: the same cores on sums of exact bfloat16 parts, error against
- * float64 no larger than float32 FMA's (a result that is not finite, or from 2^80 on, is formed by FMA). */
+ * float64 like float32 FMA's (a result that is not finite, or from 2^80 on, is formed by FMA); up to 64 rows of bf16 or 16
+ * of f32 a kernel that splits the contraction instead of the rows, f32 by FMA. */
 int switch_moe_linear_fwd(const switch_moe_linear_config* cfg, const void* x, const void* W, const float* bias,
                           const void* residual, const uint64_t* rng, void* y, void* pre, void* workspace,
                           size_t workspace_bytes, void* stream);
@@ -381,11 +382,12 @@ int switch_moe_dropout_bwd(const switch_moe_dropout_config* cfg, const void* dy,
  *   p = softmax(logits),  f_i = choices of expert i / (k n),  P_i = sum_t p[t,i] / n,  n = tokens that count,
  *   loss = mean over groups of alpha E sum_i f_i P_i      (0 for a group with n = 0). */
 typedef struct switch_moe_balance_config {
-  int32_t T, E;              /* tokens, experts (1 <= E <= 1024); T = 0 is an empty call: loss 0 */
+  int32_t T, E;              /* tokens, experts (1 <= E <= 1024); T = 0 is an empty call: loss 0; T k at most 2^30 */
   int32_t k;                 /* choices per token, 1 <= k <= min(E, 16) */
   int32_t groups;            /* 0 or 1: one; T is a multiple of it; at most 65535 */
   int32_t dtype;             /* switch_moe_dtype of logits and dlogits */
-  int32_t ld;                /* elements between rows of logits and dlogits; 0: E.  Any distance */
+  int32_t ld;                /* elements between rows of logits and dlogits; 0: E.  Any distance, and any address that
+                                suits the type; 16-byte aligned rows are read fastest */
   float alpha;
   int32_t reserved[2];       /* must be 0 */
 } switch_moe_balance_config;

@@ -11,7 +11,7 @@
 #include <cmath>
 #include <type_traits>
 
-#include "switch_common.cuh"
+#include "dropout_rng.cuh"
 
 namespace swmoe {
 namespace {
@@ -42,7 +42,7 @@ int resolve(const switch_moe_balance_config* cfg, BalanceShape* s) {
   if (!std::isfinite(c.alpha)) return SWITCH_MOE_INVALID_ARGUMENT;
   const int G = c.groups > 0 ? c.groups : 1;
   if (c.T % G != 0) return SWITCH_MOE_INVALID_ARGUMENT;
-  if (c.E > kMaxE || c.k > kMaxK || G > 65535 || (long long)c.T * c.k > 0x7fffffffll) return SWITCH_MOE_UNSUPPORTED_SHAPE;
+  if (c.E > kMaxE || c.k > kMaxK || G > 65535 || (long long)c.T * c.k > kMaxExtent) return SWITCH_MOE_UNSUPPORTED_SHAPE;
   s->T = c.T; s->E = c.E; s->k = c.k; s->G = G; s->Tg = c.T / G;
   s->ld = c.ld > 0 ? c.ld : c.E;
   s->alpha = c.alpha; s->f32 = c.dtype == SWITCH_MOE_F32;

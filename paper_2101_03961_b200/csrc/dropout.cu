@@ -148,6 +148,7 @@ int run(const switch_moe_dropout_config* cfg, const void* x, const void* res, co
   if (q < 0 || c.site < 0 || c.site > 65535) return SWITCH_MOE_INVALID_ARGUMENT;
   const long long elt = c.dtype == SWITCH_MOE_BF16 ? 2 : 4, ld = c.ld > 0 ? c.ld : c.cols;
   if (c.rows > 1 && ld * elt % 16 != 0) return SWITCH_MOE_UNSUPPORTED_SHAPE;
+  if (c.rows > kMaxExtent || c.cols > kMaxExtent) return SWITCH_MOE_UNSUPPORTED_SHAPE;
   if ((long long)c.rows * (((long long)c.cols + 7) / 8) >= 1ll << 48) return SWITCH_MOE_UNSUPPORTED_SHAPE;
   if (c.rows == 0) return SWITCH_MOE_OK;
   if (x == nullptr || y == nullptr || (q > 0 && rng == nullptr)) return SWITCH_MOE_INVALID_ARGUMENT;

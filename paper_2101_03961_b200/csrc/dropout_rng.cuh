@@ -9,6 +9,7 @@
 namespace swmoe {
 
 constexpr float kDropoutUnit = 65536.f;
+constexpr int kMaxExtent = 1 << 30;     // of a dimension: places in a tile or a step past the last one still fit 32 bits
 
 struct DropoutParams {
   const unsigned long long* rng;   // DEVICE {key, offset}; null: no dropout

@@ -42,6 +42,7 @@ int resolve(const switch_moe_linear_config* cfg, bool backward, LinearShape* s) 
   s->ldw = c.ldw > 0 ? c.ldw : c.N;
   s->ldy = c.ldy > 0 ? c.ldy : c.N;
   if (s->ldx * s->elt % 16 != 0 || s->ldw * s->elt % 16 != 0 || s->ldy * s->elt % 16 != 0) return SWITCH_MOE_UNSUPPORTED_SHAPE;
+  if (c.M > kMaxExtent || c.K > kMaxExtent || c.N > kMaxExtent) return SWITCH_MOE_UNSUPPORTED_SHAPE;
   s->ldn = ((long long)c.N + 7) / 8 * 8;
   s->ldk = ((long long)c.K + 7) / 8 * 8;
   if ((long long)c.M * (s->ldn / 8) >= 1ll << 48) return SWITCH_MOE_UNSUPPORTED_SHAPE;

@@ -192,7 +192,7 @@ def lib():
     (dict(groups=3), sm.INVALID_ARGUMENT), (dict(groups=-1), sm.INVALID_ARGUMENT), (dict(dtype=2), sm.INVALID_ARGUMENT),
     (dict(ld=7), sm.INVALID_ARGUMENT), (dict(ld=-8), sm.INVALID_ARGUMENT), (dict(alpha=float("nan")), sm.INVALID_ARGUMENT),
     (dict(E=1025), sm.UNSUPPORTED_SHAPE), (dict(E=64, k=17), sm.UNSUPPORTED_SHAPE), (dict(T=2**30, groups=2**17), sm.UNSUPPORTED_SHAPE),
-    (dict(T=2**30, k=2), sm.UNSUPPORTED_SHAPE),
+    (dict(T=2**30, k=2), sm.UNSUPPORTED_SHAPE), (dict(T=2**30 + 1), sm.UNSUPPORTED_SHAPE),
 ])
 def test_bad_configs_are_refused(lib, kw, status):
     cfg = ctypes.byref(sm.make_balance_config(**{**dict(T=64, E=8), **kw}))

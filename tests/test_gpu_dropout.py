@@ -116,7 +116,8 @@ def lib():
     (dict(rows=-1), sm.INVALID_ARGUMENT), (dict(cols=0), sm.INVALID_ARGUMENT), (dict(ld=63), sm.INVALID_ARGUMENT),
     (dict(ld=-64), sm.INVALID_ARGUMENT), (dict(dtype=5), sm.INVALID_ARGUMENT), (dict(site=65536), sm.INVALID_ARGUMENT),
     (dict(rate=1.0), sm.INVALID_ARGUMENT), (dict(rate=float("nan")), sm.INVALID_ARGUMENT), (dict(rate=-0.5), sm.INVALID_ARGUMENT),
-    (dict(cols=60), sm.UNSUPPORTED_SHAPE), (dict(ld=68), sm.UNSUPPORTED_SHAPE), (dict(rows=0), sm.OK),
+    (dict(cols=60), sm.UNSUPPORTED_SHAPE), (dict(ld=68), sm.UNSUPPORTED_SHAPE),
+    (dict(rows=2**30 + 1), sm.UNSUPPORTED_SHAPE), (dict(cols=2**30 + 64), sm.UNSUPPORTED_SHAPE), (dict(rows=0), sm.OK),
 ])
 def test_bad_configs_are_refused(lib, kw, status):
     cfg = sm.make_dropout_config(**{**dict(rows=32, cols=64, rate=0.1), **kw})

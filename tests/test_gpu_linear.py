@@ -342,6 +342,7 @@ def lib():
     (dict(ldx=56), sm.INVALID_ARGUMENT), (dict(ldw=64), sm.INVALID_ARGUMENT), (dict(ldy=8), sm.INVALID_ARGUMENT),
     (dict(ldx=-8), sm.INVALID_ARGUMENT), (dict(K=65), sm.UNSUPPORTED_SHAPE), (dict(N=73), sm.UNSUPPORTED_SHAPE),
     (dict(N=73, ldw=80, ldy=76), sm.UNSUPPORTED_SHAPE), (dict(N=74, dtype=sm.F32), sm.UNSUPPORTED_SHAPE),
+    (dict(M=2**30 + 1), sm.UNSUPPORTED_SHAPE), (dict(K=2**30 + 64), sm.UNSUPPORTED_SHAPE), (dict(N=2**30 + 64), sm.UNSUPPORTED_SHAPE),
 ])
 def test_bad_configs_are_refused(lib, kw, status):
     cfg = sm.make_linear_config(**{**dict(M=32, K=64, N=72), **kw})
