@@ -1,9 +1,9 @@
 // The dense product of few rows (a decoding step): out = x W with the whole epilogue, or dx = dz W^T, up to 64 rows of
-// bfloat16 or 16 of float32.  Such a call reads W once and little else, so it is all latency and bandwidth: a tile of the
+// bfloat16 or 16 of float32 (fused multiply-adds: 31 rows, 1792 x 8064 took 101 us here, 50 as bfloat16 parts on the tensor cores).  Such a call reads W once and little else, so it is all latency and bandwidth: a tile of the
 // tensor-core kernel (256 rows, one CTA pair per 128 columns and all of the contraction) would leave most SMs without work.
 //
-// Here a block has 64 output columns and a slice of the contraction; the blocks of the other slices form a cluster with it.
-// The rows x 8 groups of eight outputs are dealt out to the cluster's blocks; each block writes its sums into the shared memory
+// Here a block has 64 output columns (32 where that leaves SMs without a block) and a slice of the contraction; the blocks of the other slices form a cluster with it.
+// The groups of eight outputs are dealt out to the cluster's blocks; each block writes its sums into the shared memory
 // of the one that finishes them, and after one cluster barrier that one adds them up in a fixed order.  64-deep pieces of W and x come in by cp.async,
 // up to kStages at a time.  bfloat16: warp-level MMAs (16 columns of W x 8 rows of x x 16 steps: with so few rows a
 // tcgen05 tile would be padding, and the loads bound it in either case); float32: fused multiply-adds.
@@ -14,7 +14,7 @@ namespace swmoe {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kCols = 64, kDepth = 64;               // output columns of a block; steps per stage
+constexpr int kDepth = 64;                           // steps per stage
 constexpr int kMaxSlices = 8;
 
 struct RowsParams {
@@ -53,11 +53,13 @@ __device__ __forceinline__ void push(uint32_t local, uint32_t cta, float v) {
 }
 
 // Where a block keeps what the others push: [source][group of its own][8], a source being a slice and a part of a block's steps.
+// A row has kRowGroups = columns / 8 groups of eight.
 struct Sums {
   uint32_t base;
-  int groups, slices;                                 // groups of eight per block
-  __device__ __forceinline__ Sums(const RowsParams& p, uint32_t at) : base(at), groups((8 * p.M + p.slices - 1) / p.slices), slices(p.slices) {}
-  // group g of the 8 M (row g / 8, columns 8 (g % 8) ..) belongs to block g % slices
+  int groups, slices;                                 // groups per block
+  __device__ __forceinline__ Sums(const RowsParams& p, int row_groups, uint32_t at)
+      : base(at), groups((row_groups * p.M + p.slices - 1) / p.slices), slices(p.slices) {}
+  // group g (row g / row_groups, columns 8 (g % row_groups) ..) belongs to block g % slices
   __device__ __forceinline__ void put(int source, int g, int i, float v) const {
     const int own = g / slices;
     push(base + (uint32_t)(((source * groups + own) * 8 + i) * 4), (uint32_t)(g - own * slices), v);
@@ -65,9 +67,9 @@ struct Sums {
 };
 
 // What this thread's first eight results need from memory, on its way to L2 while the weights come in.
-template <typename ET>
+template <typename ET, int kRowGroups>
 __device__ __forceinline__ void prefetch_epilogue(const RowsParams& p, int rank, int col0) {
-  const int g = threadIdx.x * p.slices + rank, row = g >> 3, col = col0 + (g & 7) * 8;
+  const int g = threadIdx.x * p.slices + rank, row = g / kRowGroups, col = col0 + g % kRowGroups * 8;
   if (row >= p.M || col >= p.N) return;
   if (p.e.bias != nullptr) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.e.bias + col));
   if (p.e.residual != nullptr)
@@ -75,14 +77,14 @@ __device__ __forceinline__ void prefetch_epilogue(const RowsParams& p, int rank,
 }
 
 // After the pushes: the groups of this block.  `sources` per slice.
-template <typename ET>
+template <typename ET, int kRowGroups>
 __device__ __forceinline__ void join_slices(const RowsParams& p, const float* sums, int sources, int rank, int col0) {
   const DropoutState rng = dropout_state(p.e.dropout);
   cluster_arrive();
   cluster_wait();
-  const int groups = (8 * p.M + p.slices - 1) / p.slices;
+  const int groups = (kRowGroups * p.M + p.slices - 1) / p.slices;
   for (int own = threadIdx.x; own < groups; own += kThreads) {
-    const int g = own * p.slices + rank, row = g >> 3, col = col0 + (g & 7) * 8;
+    const int g = own * p.slices + rank, row = g / kRowGroups, col = col0 + g % kRowGroups * 8;
     if (row >= p.M || col >= p.N) continue;
     float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
@@ -97,9 +99,10 @@ __device__ __forceinline__ void join_slices(const RowsParams& p, const float* su
 }
 
 // kNK: W is stored [output column][contraction] (dx), else [contraction][output column].  NT: tiles of eight rows of x.
-template <bool kNK, int NT>
+template <bool kNK, int NT, int kCols>
 __global__ void __launch_bounds__(kThreads)
 linear_rows_kernel(const RowsParams p) {
+  constexpr int kColGroups = kCols / 16, kParts = 8 / kColGroups, kSteps = 4 / kParts;   // warps: columns x parts of the steps
   constexpr int kWBytes = kCols * kDepth * 2, kXBytes = NT * 8 * kDepth * 2, kStage = kWBytes + kXBytes;
   constexpr int kStages = 6;
   pdl_launch_dependents();
@@ -113,18 +116,21 @@ linear_rows_kernel(const RowsParams p) {
   cluster_arrive();
   pdl_wait();
   if (p.status != nullptr && blockIdx.x == 0 && threadIdx.x < kStatusWords) p.status[threadIdx.x] = 0;
-  // Tiles have rows of 128 bytes, their 16-byte pieces exchanged by the row.
+  // Tiles have rows of 128 bytes (W's of 32 columns, [step][column]: 64), their 16-byte pieces exchanged by the row.
+  constexpr int kWRow = kNK || kCols == 64 ? 128 : 64;
+  auto w_swap = [](int r) { return kWRow == 128 ? r & 7 : (r >> 1) & 3; };
   auto fetch = [&](int s) {
     const long long k0 = (long long)(first + s) * kDepth;
     const uint32_t w_dst = smem_at(smem) + (uint32_t)(s % kStages) * kStage, x_dst = w_dst + kWBytes;
 #pragma unroll
     for (int i = 0; i < kCols * 8 / kThreads; ++i) {
-      const int at = threadIdx.x + i * kThreads, r = at >> 3, piece = at & 7;
+      const int at = threadIdx.x + i * kThreads;
+      const int r = kNK || kCols == 64 ? at >> 3 : at >> 2, piece = kNK || kCols == 64 ? at & 7 : at & 3;
       const long long outer = kNK ? (long long)col0 + r : k0 + r, inner = (kNK ? k0 : (long long)col0) + piece * 8;
       const long long outer_end = kNK ? p.N : p.K, inner_end = kNK ? p.K : p.N;
       const long long left = outer < outer_end ? inner_end - inner : 0;
       const int bytes = left >= 8 ? 16 : left > 0 ? (int)left * 2 : 0;
-      copy16(w_dst + r * 128 + ((piece ^ (r & 7)) << 4), bytes > 0 ? W + outer * p.ldw + inner : W, bytes);
+      copy16(w_dst + r * kWRow + ((piece ^ w_swap(r)) << 4), bytes > 0 ? W + outer * p.ldw + inner : W, bytes);
     }
     for (int at = threadIdx.x; at < NT * 64; at += kThreads) {
       const int r = at >> 3, piece = at & 7;
@@ -138,9 +144,8 @@ linear_rows_kernel(const RowsParams p) {
     if (s < count) fetch(s);
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
-  prefetch_epilogue<__nv_bfloat16>(p, rank, col0);
-  // warp = 16 columns x half of a stage's steps
-  const int cg = warp & 3, kh = warp >> 2;
+  prefetch_epilogue<__nv_bfloat16, kCols / 8>(p, rank, col0);
+  const int cg = warp % kColGroups, kh = warp / kColGroups;
   float acc[NT][4];
 #pragma unroll
   for (int t = 0; t < NT; ++t)
@@ -153,15 +158,15 @@ linear_rows_kernel(const RowsParams p) {
     asm volatile("cp.async.commit_group;" ::: "memory");
     const uint32_t w_src = smem_at(smem) + (uint32_t)(s % kStages) * kStage, x_src = w_src + kWBytes;
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      const int step = 2 * kh + ks;                   // 16 steps of the contraction: pieces 2 step and 2 step + 1 of x's rows
+    for (int ks = 0; ks < kSteps; ++ks) {
+      const int step = kSteps * kh + ks;                   // 16 steps of the contraction: pieces 2 step and 2 step + 1 of x's rows
       uint32_t a[4];
       if (kNK) {
         const int r = 16 * cg + (lane & 15), piece = 2 * step + (lane >> 4);
-        ldm4(w_src + r * 128 + ((piece ^ (r & 7)) << 4), a);
+        ldm4(w_src + r * kWRow + ((piece ^ w_swap(r)) << 4), a);
       } else {
         const int r = 16 * step + (lane & 7) + ((lane >> 4) << 3), piece = 2 * cg + ((lane >> 3) & 1);
-        ldm4_trans(w_src + r * 128 + ((piece ^ (r & 7)) << 4), a);
+        ldm4_trans(w_src + r * kWRow + ((piece ^ w_swap(r)) << 4), a);
       }
       if constexpr (NT == 1) {
         uint32_t b[4];                                // (two of the four matrices are the same)
@@ -180,22 +185,23 @@ linear_rows_kernel(const RowsParams p) {
       }
     }
   }
-  const Sums sums(p, smem_at(smem) + kStages * kStage);
+  const Sums sums(p, kCols / 8, smem_at(smem) + kStages * kStage);
   cluster_wait();                                     // every block of the cluster is there to be written to
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int row = 8 * t + 2 * (lane & 3) + (i & 1), group = 2 * cg + (i >> 1);
-      if (row < p.M) sums.put(2 * rank + kh, 8 * row + group, lane >> 2, acc[t][i]);
+      if (row < p.M) sums.put(kParts * rank + kh, kCols / 8 * row + group, lane >> 2, acc[t][i]);
     }
-  join_slices<__nv_bfloat16>(p, reinterpret_cast<const float*>(smem + kStages * kStage), 2, rank, col0);
+  join_slices<__nv_bfloat16, kCols / 8>(p, reinterpret_cast<const float*>(smem + kStages * kStage), kParts, rank, col0);
 }
 
-// float32: thread = one column x a quarter of a stage's steps, MT rows in registers.
-template <bool kNK, int MT>
+// float32: thread = one column x a part of a stage's steps, MT rows in registers.
+template <bool kNK, int MT, int kCols>
 __global__ void __launch_bounds__(kThreads)
 linear_rows_f32_kernel(const RowsParams p) {
+  constexpr int kParts = kThreads / kCols, kSteps = kDepth / kParts;
   constexpr int kWBytes = kCols * kDepth * 4, kXBytes = MT * kDepth * 4, kStage = kWBytes + kXBytes;
   constexpr int kStages = 4;
   pdl_launch_dependents();
@@ -208,18 +214,21 @@ linear_rows_f32_kernel(const RowsParams p) {
   cluster_arrive();
   pdl_wait();
   if (p.status != nullptr && blockIdx.x == 0 && threadIdx.x < kStatusWords) p.status[threadIdx.x] = 0;
-  // W's tile has rows of 256 bytes, their 16-byte pieces exchanged by the row where lanes read down a column of pieces.
+  // W's tile has rows of 64 steps or kCols columns, their 16-byte pieces exchanged by the row where lanes read down a column of
+  // pieces.
+  constexpr int kWRow = kNK ? kDepth * 4 : kCols * 4;
   auto fetch = [&](int s) {
     const long long k0 = (long long)(first + s) * kDepth;
     const uint32_t w_dst = smem_at(smem) + (uint32_t)(s % kStages) * kStage, x_dst = w_dst + kWBytes;
 #pragma unroll
     for (int i = 0; i < kCols * 16 / kThreads; ++i) {
-      const int at = threadIdx.x + i * kThreads, r = at >> 4, piece = at & 15;
+      const int at = threadIdx.x + i * kThreads;
+      const int r = kNK || kCols == 64 ? at >> 4 : at >> 3, piece = kNK || kCols == 64 ? at & 15 : at & 7;
       const long long outer = kNK ? (long long)col0 + r : k0 + r, inner = (kNK ? k0 : (long long)col0) + piece * 4;
       const long long outer_end = kNK ? p.N : p.K, inner_end = kNK ? p.K : p.N;
       const long long left = outer < outer_end ? inner_end - inner : 0;
       const int bytes = left >= 4 ? 16 : left > 0 ? (int)left * 4 : 0;
-      copy16(w_dst + r * 256 + ((kNK ? piece ^ (r & 15) : piece) << 4), bytes > 0 ? W + outer * p.ldw + inner : W, bytes);
+      copy16(w_dst + r * kWRow + ((kNK ? piece ^ (r & 15) : piece) << 4), bytes > 0 ? W + outer * p.ldw + inner : W, bytes);
     }
     for (int at = threadIdx.x; at < MT * 16; at += kThreads) {
       const int r = at >> 4, piece = at & 15;
@@ -233,8 +242,8 @@ linear_rows_f32_kernel(const RowsParams p) {
     if (s < count) fetch(s);
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
-  prefetch_epilogue<float>(p, rank, col0);
-  const int c = threadIdx.x & 63, kq = threadIdx.x >> 6;
+  prefetch_epilogue<float, kCols / 8>(p, rank, col0);
+  const int c = threadIdx.x % kCols, kq = threadIdx.x / kCols;
   float acc[MT];
 #pragma unroll
   for (int m = 0; m < MT; ++m) acc[m] = 0.f;
@@ -246,15 +255,15 @@ linear_rows_f32_kernel(const RowsParams p) {
     const uint8_t* w_src = smem + (s % kStages) * kStage;
     const uint8_t* x_src = w_src + kWBytes;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {                     // four steps at a time
-      const int k = 16 * kq + 4 * q;
+    for (int q = 0; q < kSteps / 4; ++q) {            // four steps at a time
+      const int k = kSteps * kq + 4 * q;
       float w[4];
       if (kNK) {
-        const float4 v = *reinterpret_cast<const float4*>(w_src + c * 256 + (((k >> 2) ^ (c & 15)) << 4));
+        const float4 v = *reinterpret_cast<const float4*>(w_src + c * kWRow + (((k >> 2) ^ (c & 15)) << 4));
         w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
       } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const float*>(w_src + (k + i) * 256 + c * 4);
+        for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const float*>(w_src + (k + i) * kWRow + c * 4);
       }
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
@@ -266,16 +275,16 @@ linear_rows_f32_kernel(const RowsParams p) {
       }
     }
   }
-  const Sums sums(p, smem_at(smem) + kStages * kStage);
+  const Sums sums(p, kCols / 8, smem_at(smem) + kStages * kStage);
   cluster_wait();
 #pragma unroll
   for (int m = 0; m < MT; ++m)
-    if (m < p.M) sums.put(4 * rank + kq, 8 * m + (c >> 3), c & 7, acc[m]);
-  join_slices<float>(p, reinterpret_cast<const float*>(smem + kStages * kStage), 4, rank, col0);
+    if (m < p.M) sums.put(kParts * rank + kq, kCols / 8 * m + (c >> 3), c & 7, acc[m]);
+  join_slices<float, kCols / 8>(p, reinterpret_cast<const float*>(smem + kStages * kStage), kParts, rank, col0);
 }
 
 template <typename Kern>
-int launch(Kern kernel, size_t smem, int slices, const RowsParams& p, bool* ready, cudaStream_t st) {
+int launch(Kern kernel, size_t smem, int cols, const RowsParams& p, bool* ready, cudaStream_t st) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return SWITCH_MOE_CUDA_ERROR;
   if (dev < 0 || dev >= 64 || !ready[dev]) {
@@ -283,7 +292,7 @@ int launch(Kern kernel, size_t smem, int slices, const RowsParams& p, bool* read
     if (dev >= 0 && dev < 64) ready[dev] = true;
   }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(((p.N + (long long)kCols - 1) / kCols) * slices));
+  cfg.gridDim = dim3((unsigned)(((p.N + (long long)cols - 1) / cols) * p.slices));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
@@ -291,7 +300,7 @@ int launch(Kern kernel, size_t smem, int slices, const RowsParams& p, bool* read
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)slices;
+  attr[1].val.clusterDim.x = (unsigned)p.slices;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
@@ -299,25 +308,30 @@ int launch(Kern kernel, size_t smem, int slices, const RowsParams& p, bool* read
   return launch_status();
 }
 
-template <bool kNK, int NT>
+// Shared memory: the stages, then for every source the groups of eight of this block (rounded up).
+constexpr size_t sum_bytes(int parts, int rows, int cols) { return (size_t)parts * (rows * cols / 8 + kMaxSlices) * 32; }
+
+template <bool kNK, int NT, int kCols>
 int launch_bf16(const RowsParams& p, cudaStream_t st) {
   static bool ready[64] = {false};
-  // stages, then two sums a slice for every output (the groups per block rounded up)
-  return launch(linear_rows_kernel<kNK, NT>, (size_t)6 * (kCols * kDepth * 2 + NT * 8 * kDepth * 2) + 2 * (NT * 8 * 8 + kMaxSlices) * 32,
-                p.slices, p, ready, st);
+  return launch(linear_rows_kernel<kNK, NT, kCols>,
+                (size_t)6 * (kCols * kDepth * 2 + NT * 8 * kDepth * 2) + sum_bytes(8 / (kCols / 16), NT * 8, kCols), kCols, p, ready, st);
 }
-template <bool kNK, int MT>
+template <bool kNK, int MT, int kCols>
 int launch_f32(const RowsParams& p, cudaStream_t st) {
   static bool ready[64] = {false};
-  return launch(linear_rows_f32_kernel<kNK, MT>, (size_t)4 * (kCols * kDepth * 4 + MT * kDepth * 4) + 4 * (MT * 8 + kMaxSlices) * 32,
-                p.slices, p, ready, st);
+  return launch(linear_rows_f32_kernel<kNK, MT, kCols>,
+                (size_t)4 * (kCols * kDepth * 4 + MT * kDepth * 4) + sum_bytes(kThreads / kCols, MT, kCols), kCols, p, ready, st);
 }
-template <bool kNK>
-int launch_any(const DenseProduct& q, const RowsParams& p, cudaStream_t st) {
-  if (q.f32) return q.rows <= 4 ? launch_f32<kNK, 4>(p, st) : launch_f32<kNK, 16>(p, st);
-  if (q.rows <= 8) return launch_bf16<kNK, 1>(p, st);
-  if (q.rows <= 16) return launch_bf16<kNK, 2>(p, st);
-  return q.rows <= 32 ? launch_bf16<kNK, 4>(p, st) : launch_bf16<kNK, 8>(p, st);
+template <bool kNK, int kCols>
+int launch_cols(const DenseProduct& q, const RowsParams& p, cudaStream_t st) {
+  if (q.f32) {
+    if (q.rows <= 4) return launch_f32<kNK, 4, kCols>(p, st);
+    return launch_f32<kNK, 16, kCols>(p, st);
+  }
+  if (q.rows <= 8) return launch_bf16<kNK, 1, kCols>(p, st);
+  if (q.rows <= 16) return launch_bf16<kNK, 2, kCols>(p, st);
+  return q.rows <= 32 ? launch_bf16<kNK, 4, kCols>(p, st) : launch_bf16<kNK, 8, kCols>(p, st);
 }
 
 }  // namespace
@@ -329,15 +343,21 @@ int launch_dense_rows(DenseKind kind, const DenseProduct& q, const DenseEpilogue
   p.x = q.a.p; p.W = q.b.p; p.ldx = q.a.ld; p.ldw = q.b.ld; p.ld_out = q.ld_out;
   p.M = q.rows; p.N = q.cols; p.K = q.k; p.e = e; p.out = q.out;
   p.status = q.clear_status ? q.status : nullptr;
-  const long long blocks = ((long long)q.cols + kCols - 1) / kCols, stages = ((long long)q.k + kDepth - 1) / kDepth;
-  long long slices = 2 * kChipSms / blocks;
-  if (slices > kMaxSlices) slices = kMaxSlices;
-  if (slices > stages) slices = stages;
-  if (slices < 1) slices = 1;
+  const long long stages = ((long long)q.k + kDepth - 1) / kDepth;
+  auto slices_for = [&](long long blocks) {
+    long long slices = 2 * kChipSms / blocks;
+    if (slices > kMaxSlices) slices = kMaxSlices;
+    if (slices > stages) slices = stages;
+    return slices < 1 ? 1ll : slices;
+  };
+  const long long wide = ((long long)q.cols + 63) / 64;
+  const bool narrow = wide * slices_for(wide) < kChipSms;
+  const long long blocks = narrow ? ((long long)q.cols + 31) / 32 : wide, slices = slices_for(blocks);
   p.depth_per_slice = (int)((stages + slices - 1) / slices);
   p.slices = (int)((stages + p.depth_per_slice - 1) / p.depth_per_slice);
   if (blocks * p.slices > 0x7fffffffll) return SWITCH_MOE_UNSUPPORTED_SHAPE;
-  return kind == kDenseDx ? launch_any<true>(q, p, st) : launch_any<false>(q, p, st);
+  if (kind == kDenseDx) return narrow ? launch_cols<true, 32>(q, p, st) : launch_cols<true, 64>(q, p, st);
+  return narrow ? launch_cols<false, 32>(q, p, st) : launch_cols<false, 64>(q, p, st);
 }
 
 }  // namespace swmoe
