@@ -18,7 +18,8 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxE = 1024, kMaxK = 16;
-constexpr int kFinalExperts = 32;                    // experts per block of the second kernel
+constexpr int kFinalExperts = 32;                    // experts per block of the second kernel, of
+constexpr int kFinalThreads = 1024, kFinalWarps = kFinalThreads / 32;
 
 struct BalanceShape {
   int T, E, k, G, Tg, blocks;      // blocks per group
@@ -46,8 +47,8 @@ int resolve(const switch_moe_balance_config* cfg, BalanceShape* s) {
   s->T = c.T; s->E = c.E; s->k = c.k; s->G = G; s->Tg = c.T / G;
   s->ld = c.ld > 0 ? c.ld : c.E;
   s->alpha = c.alpha; s->f32 = c.dtype == SWITCH_MOE_F32;
-  // about four blocks per SM over all groups, each with 8 rows a warp or more
-  long long want = ((long long)4 * kChipSms + G - 1) / G, most = (s->Tg + 8 * kWarps - 1) / (8 * kWarps);
+  // about two blocks per SM over all groups (what its registers allow at once), each with 8 rows a warp or more
+  long long want = ((long long)2 * kChipSms + G - 1) / G, most = (s->Tg + 8 * kWarps - 1) / (8 * kWarps);
   s->blocks = (int)(want < most ? want : most);
   if (s->blocks < 1) s->blocks = 1;
   s->alone = false;                // (decided where the layout is known)
@@ -203,18 +204,23 @@ balance_rows_kernel(const ET* logits, const int* index, const uint8_t* mask, Bal
   const int stride = (int)gridDim.x * kWarps * per_warp;
   const int first = ((int)blockIdx.x * kWarps + warp) * per_warp;
   // every lane of a warp takes the same number of steps: rows beyond the group's end are rows that do not count
-  auto fetch = [&](int t, Row<ET, V, NV>& r) {
+  auto counts = [&](int t) {
     const int at = t + lane / L;
-    const bool valid = at < s.Tg && (mask == nullptr || mask[row0 + at] != 0);
-    r.load(logits + (row0 + (valid ? at : 0)) * s.ld, valid, l, L, s.E);
-    return valid;
+    return at < s.Tg && (mask == nullptr || mask[row0 + at] != 0);
   };
+  auto fetch = [&](int t, bool valid, Row<ET, V, NV>& r) {
+    r.load(logits + (row0 + (valid ? t + lane / L : 0)) * s.ld, valid, l, L, s.E);
+  };
+  // The logits of the next step are on their way during this one, and the mask of the one after that.
   Row<ET, V, NV> next;
-  bool next_valid = first < s.Tg && fetch(first, next);
+  bool next_valid = counts(first), after_valid = counts(first + stride);
+  fetch(first, next_valid, next);
   for (int t = first; t < s.Tg; t += stride) {
     const Row<ET, V, NV> raw = next;
     const bool valid = next_valid;
-    if (t + stride < s.Tg) next_valid = fetch(t + stride, next);
+    next_valid = after_valid;
+    fetch(t + stride, next_valid, next);
+    after_valid = counts(t + 2 * stride);
     if (!__any_sync(0xffffffffu, valid)) continue;    // padding, mostly at the ends of sequences
     float m, scale, p[V * NV];
     const bool used = raw.softmax(L, p, &scale, &m) && valid;
@@ -309,21 +315,21 @@ balance_rows_kernel(const ET* logits, const int* index, const uint8_t* mask, Bal
   }
 }
 
-// Adds up the blocks of group blockIdx.y for 32 experts: warp w takes the blocks w, w + 8, ..; lane = expert.
-__global__ void __launch_bounds__(kThreads)
+// Adds up the blocks of group blockIdx.y for 32 experts: warp w takes the blocks w, w + 32, ..; lane = expert.
+__global__ void __launch_bounds__(kFinalThreads)
 balance_sum_kernel(const int* tokens_part, const int* counts_part, const float* psum_part, BalanceShape s,
                    unsigned* ticket, float* loss_part, float* loss, int* counts, int* tokens) {
   pdl_launch_dependents();
   pdl_wait();
-  __shared__ double p_s[kWarps][32];
-  __shared__ int c_s[kWarps][32], n_s[kWarps];
+  __shared__ double p_s[kFinalWarps][32];
+  __shared__ int c_s[kFinalWarps][32], n_s[kFinalWarps];
   __shared__ bool last;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = blockIdx.y;
   const int e = blockIdx.x * kFinalExperts + lane;
   double p = 0.0;                                     // (a group may have millions of tokens)
   int c = 0, n = 0;
 #pragma unroll 4
-  for (int b = warp; b < s.blocks; b += kWarps) {
+  for (int b = warp; b < s.blocks; b += kFinalWarps) {
     const long long part = (long long)g * s.blocks + b;
     if (e < s.E) {
       p += (double)psum_part[part * s.E + e];
@@ -337,7 +343,7 @@ balance_sum_kernel(const int* tokens_part, const int* counts_part, const float* 
   __syncthreads();
   if (warp == 0) {
     p = 0.0; c = 0; n = 0;
-    for (int w = 0; w < kWarps; ++w) { p += p_s[w][lane]; c += c_s[w][lane]; n += n_s[w]; }
+    for (int w = 0; w < kFinalWarps; ++w) { p += p_s[w][lane]; c += c_s[w][lane]; n += n_s[w]; }
     if (e < s.E) counts[(long long)g * s.E + e] = c;
     if (blockIdx.x == 0 && lane == 0) tokens[g] = n;
     double term = e < s.E && n > 0 ? (double)c * p : 0.0;
@@ -355,14 +361,14 @@ balance_sum_kernel(const int* tokens_part, const int* counts_part, const float* 
   // the loss: all parts, in an order that does not depend on which block came last
   const long long parts = (long long)gridDim.x * gridDim.y;
   double sum = 0.0;
-  for (long long i = threadIdx.x; i < parts; i += kThreads) sum += (double)__ldcg(loss_part + i);
+  for (long long i = threadIdx.x; i < parts; i += kFinalThreads) sum += (double)__ldcg(loss_part + i);
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   __syncthreads();
   if (lane == 0) p_s[warp][0] = sum;
   __syncthreads();
   if (threadIdx.x == 0) {
     sum = 0.0;
-    for (int w = 0; w < kWarps; ++w) sum += p_s[w][0];
+    for (int w = 0; w < kFinalWarps; ++w) sum += p_s[w][0];
     *loss = (float)(sum / s.G);
   }
 }
@@ -457,7 +463,7 @@ int forward(BalanceShape s, const BalancePlan& p, const void* logits, const int3
     return launch_status();
   });
   if (rc != SWITCH_MOE_OK || s.alone) return rc;
-  launch_k(balance_sum_kernel, dim3((s.E + kFinalExperts - 1) / kFinalExperts, s.G), dim3(kThreads), 0, st,
+  launch_k(balance_sum_kernel, dim3((s.E + kFinalExperts - 1) / kFinalExperts, s.G), dim3(kFinalThreads), 0, st,
            static_cast<const int*>(tp), static_cast<const int*>(cp), static_cast<const float*>(pp), s, ticket,
            ws_ptr<float>(ws, p.loss_part), loss, counts, tokens);
   return launch_status();

@@ -86,68 +86,6 @@ void make_plan(const LinearShape& s, bool backward, LinearPlan* p) {
   p->total = off;
 }
 
-// Eight consecutive elements of a row, the first `n` of them inside; 16-byte aligned.
-__device__ __forceinline__ void load8(const float* p, int n, float* f) {
-  if (n >= 8) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float4 v = *reinterpret_cast<const float4*>(p + 4 * i);
-      f[4 * i] = v.x; f[4 * i + 1] = v.y; f[4 * i + 2] = v.z; f[4 * i + 3] = v.w;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = i < n ? p[i] : 0.f;
-  }
-}
-// The same in flight: loaded now, converted when it is needed.
-template <typename ET> struct Raw8;
-template <> struct Raw8<__nv_bfloat16> {
-  uint4 v;
-  __device__ __forceinline__ void load(const __nv_bfloat16* p, int n) {
-    if (n >= 8) {
-      v = *reinterpret_cast<const uint4*>(p);
-    } else {
-      const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
-      uint32_t w[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = (2 * i < n ? q[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)q[2 * i + 1] << 16 : 0u);
-      v = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-  }
-  __device__ __forceinline__ void get(float* f) const {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
-  }
-};
-template <> struct Raw8<float> {
-  float f8[8];
-  __device__ __forceinline__ void load(const float* p, int n) { load8(p, n, f8); }
-  __device__ __forceinline__ void get(float* f) const {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = f8[i];
-  }
-};
-__device__ __forceinline__ void store8(__nv_bfloat16* p, int n, const float* f) {
-  if (n >= 8) {
-    uint4 v;
-    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-    *reinterpret_cast<uint4*>(p) = v;
-  } else {
-    for (int i = 0; i < n; ++i) p[i] = __float2bfloat16(f[i]);
-  }
-}
-__device__ __forceinline__ void store8(float* p, int n, const float* f) {
-  if (n >= 8) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      *reinterpret_cast<float4*>(p + 4 * i) = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
-  } else {
-    for (int i = 0; i < n; ++i) p[i] = f[i];
-  }
-}
 // x 2^24 = h + m + l: three arrays `plane` elements apart.  (A value beyond the parts' range makes m NaN, and with it the
 // results that it meets, which the product then forms again.)
 __device__ __forceinline__ void store_parts8(__nv_bfloat16* p, long long plane, const float* f) {
@@ -207,22 +145,8 @@ linear_dz_kernel(const ET* __restrict__ dy, const ET* __restrict__ pre, DzArgs a
         if (row >= row_end) break;
         float g[8], z[8];
         graw[k].get(g);
-        if (a.dropout.rng != nullptr) {
-          const uint4 bits = dropout_bits(a.dropout, rng, (unsigned long long)row * (unsigned)a.per_row + (unsigned)(col >> 3));
-        dropout8(a.dropout, bits, g);
-        }
         if (kAct != SWITCH_MOE_ACT_NONE) zraw[k].get(z);
-        if (kAct == SWITCH_MOE_ACT_RELU) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) g[i] = z[i] > 0.f ? g[i] : 0.f;
-        } else if (kAct == SWITCH_MOE_ACT_GELU) {
-#pragma unroll
-          for (int i = 0; i < 8; i += 2) {
-            const float2 d = gelu_grad_pair(z[i], z[i + 1]);
-            g[i] *= d.x;
-            g[i + 1] *= d.y;
-          }
-        }
+        dz8(kAct, a.dropout, rng, (unsigned long long)row * (unsigned)a.per_row + (unsigned)(col >> 3), z, g);
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[i] += g[i];
         if (dz != nullptr) store8(dz + row * a.ldn + col, 8, g);        // (the workspace's rows are multiples of 8)
@@ -431,6 +355,27 @@ extern "C" int switch_moe_linear_bwd(const switch_moe_linear_config* cfg, const 
   if (dy == nullptr || (dW != nullptr && x == nullptr) || (dx != nullptr && W == nullptr) ||
       (s.act != SWITCH_MOE_ACT_NONE && pre == nullptr) || (s.q > 0 && rng == nullptr))
     return SWITCH_MOE_INVALID_ARGUMENT;
+  if (s.rows_kernel && rows_dw_pays(s.M, s.K, s.N)) {
+    // few rows: dW, the bias gradient and, for dx, dz itself in one launch (what is not wanted is left out, so that the rest
+    // comes out the same)
+    const bool keep_dz = dx != nullptr && (s.act != SWITCH_MOE_ACT_NONE || s.q > 0);
+    RowsDw d{};
+    d.dy = dy; d.pre = pre; d.x = x; d.dW = dW; d.dbias = dbias; d.dz = keep_dz ? ws_ptr<void>(workspace, p.dz) : nullptr;
+    d.M = s.M; d.K = s.K; d.N = s.N; d.act = s.act; d.per_row = (int)(s.ldn / 8);
+    d.ldx = s.ldx; d.ldw = s.ldw; d.ldy = s.ldy; d.ldn = s.ldn;
+    d.round_dz = s.act != SWITCH_MOE_ACT_NONE || s.q > 0;
+    d.dropout = dropout_params(rng, s.q, s.site);
+    d.status = status;
+    const bool any = dW != nullptr || dbias != nullptr || keep_dz;
+    if (any) SWMOE_TRY(launch_rows_dw(s.f32, d, st));
+    if (dx == nullptr) return SWITCH_MOE_OK;
+    DenseProduct q{};
+    q.rows = s.M; q.cols = s.K; q.k = s.N; q.f32 = s.f32;
+    q.a.p = keep_dz ? d.dz : dy; q.a.ld = keep_dz ? s.ldn : s.ldy;
+    q.b.p = W; q.b.ld = s.ldw;
+    q.out = dx; q.ld_out = s.ldx; q.status = status; q.clear_status = !any;
+    return launch_dense_rows(kDenseDx, q, DenseEpilogue{}, st);
+  }
   const bool products = dx != nullptr || dW != nullptr, own_dz = s.act != SWITCH_MOE_ACT_NONE || s.q > 0;
   bool cleared = false;
   void* dz = own_dz && products ? ws_ptr<void>(workspace, p.dz) : nullptr;

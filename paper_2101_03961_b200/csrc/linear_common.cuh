@@ -47,6 +47,19 @@ int launch_dense_rows(DenseKind kind, const DenseProduct& q, const DenseEpilogue
 struct DenseTiling {
   int splits, width;
 };
+// Weight and bias gradient of few rows, with dz kept for dx (linear_rows.cu).
+struct RowsDw {
+  const void* dy; const void* pre; const void* x;
+  void* dW; float* dbias; void* dz;
+  int M, K, N, act, per_row;
+  long long ldx, ldw, ldy, ldn;
+  bool round_dz;                   // dz is rounded to the activation type before it is multiplied
+  DropoutParams dropout;
+  int* status;
+};
+// Its fused multiply-adds take 1 us per 36 million; the tensor-core product, its pass over dz and their launches 10 us more.
+inline bool rows_dw_pays(long long M, long long K, long long N) { return M * K * N <= 300000000ll && K <= 1 << 20; }
+int launch_rows_dw(bool f32, const RowsDw& d, cudaStream_t st);
 DenseTiling dense_tiling(DenseKind kind, bool f32, long long rows, long long cols, long long k);
 int launch_dense(DenseKind kind, const DenseProduct& q, const DenseEpilogue& e, cudaStream_t st);
 
@@ -184,6 +197,85 @@ __device__ __forceinline__ void finish8(const DenseEpilogue& e, const DropoutSta
       if (i < n) x[i] += (float)r[i];
   }
   put(out, x);
+}
+
+// Eight consecutive elements of a row, the first `n` of them inside; 16-byte aligned.
+__device__ __forceinline__ void load8(const float* p, int n, float* f) {
+  if (n >= 8) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float4 v = *reinterpret_cast<const float4*>(p + 4 * i);
+      f[4 * i] = v.x; f[4 * i + 1] = v.y; f[4 * i + 2] = v.z; f[4 * i + 3] = v.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = i < n ? p[i] : 0.f;
+  }
+}
+// The same in flight: loaded now, converted when it is needed.
+template <typename ET> struct Raw8;
+template <> struct Raw8<__nv_bfloat16> {
+  uint4 v;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p, int n) {
+    if (n >= 8) {
+      v = *reinterpret_cast<const uint4*>(p);
+    } else {
+      const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = (2 * i < n ? q[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)q[2 * i + 1] << 16 : 0u);
+      v = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+  __device__ __forceinline__ void get(float* f) const {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+  }
+};
+template <> struct Raw8<float> {
+  float f8[8];
+  __device__ __forceinline__ void load(const float* p, int n) { load8(p, n, f8); }
+  __device__ __forceinline__ void get(float* f) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = f8[i];
+  }
+};
+__device__ __forceinline__ void store8(__nv_bfloat16* p, int n, const float* f) {
+  if (n >= 8) {
+    uint4 v;
+    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+    *reinterpret_cast<uint4*>(p) = v;
+  } else {
+    for (int i = 0; i < n; ++i) p[i] = __float2bfloat16(f[i]);
+  }
+}
+__device__ __forceinline__ void store8(float* p, int n, const float* f) {
+  if (n >= 8) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      *reinterpret_cast<float4*>(p + 4 * i) = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+  } else {
+    for (int i = 0; i < n; ++i) p[i] = f[i];
+  }
+}
+// Eight values of dy become those of dz = dropout(dy) . activation'(z); `block` is their place in the dropout's count.
+__device__ __forceinline__ void dz8(int act, const DropoutParams& dropout, const DropoutState& rng, unsigned long long block,
+                                    const float* z, float* g) {
+  if (dropout.rng != nullptr) dropout8(dropout, dropout_bits(dropout, rng, block), g);
+  if (act == SWITCH_MOE_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g[i] = z[i] > 0.f ? g[i] : 0.f;
+  } else if (act == SWITCH_MOE_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      const float2 d = gelu_grad_pair(z[i], z[i + 1]);
+      g[i] *= d.x;
+      g[i + 1] *= d.y;
+    }
+  }
 }
 
 }  // namespace swmoe

@@ -283,6 +283,99 @@ linear_rows_f32_kernel(const RowsParams p) {
   join_slices<float, kCols / 8>(p, reinterpret_cast<const float*>(smem + kStages * kStage), kParts, rank, col0);
 }
 
+// dW = x^T dz of up to 64 rows, by fused multiply-adds: a block has 64 rows x 128 columns of dW, a thread 4 x 8 of them, and
+// forms its columns' dz itself; the blocks of the first 64 rows also leave the bias gradient, and dz for the product of dx
+// (they alone, where dW is not wanted).
+// Bound by writing dW, and by the launches that it saves.
+constexpr int kDwRows = 64, kDwCols = 128, kDwPitch = kDwCols + 4;
+template <typename ET>
+__global__ void __launch_bounds__(kThreads)
+linear_rows_dw_kernel(const RowsDw p) {
+  pdl_launch_dependents();
+  extern __shared__ __align__(16) float tile[];       // x [M][64], then dz [M][128 + 4]
+  pdl_wait();
+  if (p.status != nullptr && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < kStatusWords) p.status[threadIdx.x] = 0;
+  float* const xs = tile;
+  float* const gs = tile + p.M * kDwRows;
+  const ET* x = static_cast<const ET*>(p.x);
+  const ET* dy = static_cast<const ET*>(p.dy);
+  const ET* pre = static_cast<const ET*>(p.pre);
+  const long long col0 = (long long)blockIdx.x * kDwCols, k0 = (long long)blockIdx.y * kDwRows;
+  const DropoutState rng = dropout_state(p.dropout);
+  for (int u = threadIdx.x; p.dW != nullptr && u < p.M * (kDwRows / 8); u += kThreads) {
+    const int row = u / (kDwRows / 8), c = u % (kDwRows / 8) * 8;
+    const long long left = p.K - (k0 + c);
+    float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (left > 0) {
+      Raw8<ET> raw;
+      raw.load(x + row * p.ldx + k0 + c, left < 8 ? (int)left : 8);
+      raw.get(f);
+    }
+    store8(xs + row * kDwRows + c, 8, f);
+  }
+  const bool sums = blockIdx.y == 0 && p.dbias != nullptr;
+  for (int u = threadIdx.x; u < p.M * (kDwCols / 8); u += kThreads) {
+    const int row = u / (kDwCols / 8), c = u % (kDwCols / 8) * 8;
+    const long long left = p.N - (col0 + c);
+    float g[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (left > 0) {
+      const int n = left < 8 ? (int)left : 8;
+      Raw8<ET> graw, zraw;
+      float z[8];
+      graw.load(dy + row * p.ldy + col0 + c, n);
+      if (p.act != SWITCH_MOE_ACT_NONE) zraw.load(pre + row * p.ldy + col0 + c, n);
+      graw.get(g);
+      if (p.act != SWITCH_MOE_ACT_NONE) zraw.get(z);
+      dz8(p.act, p.dropout, rng, (unsigned long long)row * (unsigned)p.per_row + (unsigned)((col0 + c) >> 3), z, g);
+      if (p.dz != nullptr && blockIdx.y == 0) store8(static_cast<ET*>(p.dz) + row * p.ldn + col0 + c, 8, g);
+    }
+    if (sizeof(ET) == 2 && p.round_dz && !sums) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[i] = __bfloat162float(__float2bfloat16(g[i]));
+    }
+    store8(gs + row * kDwPitch + c, 8, g);
+  }
+  __syncthreads();
+  if (sums) {                                          // of dz as it is, before it is rounded
+    if (threadIdx.x < kDwCols && col0 + threadIdx.x < p.N) {
+      float s = 0.f;
+      for (int m = 0; m < p.M; ++m) s += gs[m * kDwPitch + threadIdx.x];
+      p.dbias[col0 + threadIdx.x] = s;
+    }
+    __syncthreads();
+    if (sizeof(ET) == 2 && p.round_dz)
+      for (int u = threadIdx.x; u < p.M * kDwCols; u += kThreads) {
+        float* at = gs + u / kDwCols * kDwPitch + u % kDwCols;
+        *at = __bfloat162float(__float2bfloat16(*at));
+      }
+    __syncthreads();
+  }
+  if (p.dW == nullptr) return;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;                // columns 8 tx .., rows 4 ty ..
+  float acc[4][8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[i][j] = 0.f;
+#pragma unroll 2
+  for (int m = 0; m < p.M; ++m) {
+    const float4 a = *reinterpret_cast<const float4*>(xs + m * kDwRows + 4 * ty);
+    float b[8];
+    load8(gs + m * kDwPitch + 8 * tx, 8, b);
+    const float av[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[i][j] = fmaf(av[i], b[j], acc[i][j]);
+  }
+  const long long n = p.N - (col0 + 8 * tx);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const long long k = k0 + 4 * ty + i;
+    if (k < p.K && n > 0) store8(static_cast<ET*>(p.dW) + k * p.ldw + col0 + 8 * tx, n < 8 ? (int)n : 8, acc[i]);
+  }
+}
+
 template <typename Kern>
 int launch(Kern kernel, size_t smem, int cols, const RowsParams& p, bool* ready, cudaStream_t st) {
   int dev = 0;
@@ -358,6 +451,22 @@ int launch_dense_rows(DenseKind kind, const DenseProduct& q, const DenseEpilogue
   if (blocks * p.slices > 0x7fffffffll) return SWITCH_MOE_UNSUPPORTED_SHAPE;
   if (kind == kDenseDx) return narrow ? launch_cols<true, 32>(q, p, st) : launch_cols<true, 64>(q, p, st);
   return narrow ? launch_cols<false, 32>(q, p, st) : launch_cols<false, 64>(q, p, st);
+}
+
+int launch_rows_dw(bool f32, const RowsDw& d, cudaStream_t st) {
+  const size_t smem = (size_t)d.M * (kDwRows + kDwPitch) * 4;        // 64 rows: 50 KB
+  static bool ready[2][64] = {};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return SWITCH_MOE_CUDA_ERROR;
+  auto kernel = f32 ? linear_rows_dw_kernel<float> : linear_rows_dw_kernel<__nv_bfloat16>;
+  if (dev < 0 || dev >= 64 || !ready[f32][dev]) {
+    const int most = 64 * (kDwRows + kDwPitch) * 4;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess) return SWITCH_MOE_CUDA_ERROR;
+    if (dev >= 0 && dev < 64) ready[f32][dev] = true;
+  }
+  const long long by = d.dW != nullptr ? ((long long)d.K + kDwRows - 1) / kDwRows : 1;
+  launch_k(kernel, dim3((unsigned)(((long long)d.N + kDwCols - 1) / kDwCols), (unsigned)by), dim3(kThreads), smem, st, d);
+  return launch_status();
 }
 
 }  // namespace swmoe
