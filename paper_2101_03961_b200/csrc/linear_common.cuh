@@ -57,8 +57,9 @@ struct RowsDw {
   DropoutParams dropout;
   int* status;
 };
-// Its fused multiply-adds take 1 us per 36 million; the tensor-core product, its pass over dz and their launches 10 us more.
-inline bool rows_dw_pays(long long M, long long K, long long N) { return M * K * N <= 300000000ll && K <= 1 << 20; }
+// Up to where one launch takes less than the pass over dz and the tensor-core product (us: 16 rows, 512 x 2880 14 against 21,
+// 40 rows, 576 x 2752 31 and 31, 13 rows, 1008 x 7506 27 and 26).
+inline bool rows_dw_pays(long long M, long long K, long long N) { return M * K * N <= 50000000ll; }
 int launch_rows_dw(bool f32, const RowsDw& d, cudaStream_t st);
 DenseTiling dense_tiling(DenseKind kind, bool f32, long long rows, long long cols, long long k);
 int launch_dense(DenseKind kind, const DenseProduct& q, const DenseEpilogue& e, cudaStream_t st);

@@ -16,6 +16,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kDepth = 64;                           // steps per stage
 constexpr int kMaxSlices = 8;
+constexpr int kStages = 6, kStagesF32 = 4;           // ring in shared memory
 
 struct RowsParams {
   const void* x; const void* W;
@@ -23,6 +24,7 @@ struct RowsParams {
   int M, N;                        // rows, output columns
   long long K;
   int slices, depth_per_slice;     // in stages of kDepth
+  int stages;                      // that shared memory holds: all of a slice's, up to a ring of kStages
   DenseEpilogue e;
   void* out;
   int* status;
@@ -104,7 +106,6 @@ __global__ void __launch_bounds__(kThreads)
 linear_rows_kernel(const RowsParams p) {
   constexpr int kColGroups = kCols / 16, kParts = 8 / kColGroups, kSteps = 4 / kParts;   // warps: columns x parts of the steps
   constexpr int kWBytes = kCols * kDepth * 2, kXBytes = NT * 8 * kDepth * 2, kStage = kWBytes + kXBytes;
-  constexpr int kStages = 6;
   pdl_launch_dependents();
   extern __shared__ __align__(1024) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -185,7 +186,7 @@ linear_rows_kernel(const RowsParams p) {
       }
     }
   }
-  const Sums sums(p, kCols / 8, smem_at(smem) + kStages * kStage);
+  const Sums sums(p, kCols / 8, smem_at(smem) + p.stages * kStage);
   cluster_wait();                                     // every block of the cluster is there to be written to
 #pragma unroll
   for (int t = 0; t < NT; ++t)
@@ -194,7 +195,7 @@ linear_rows_kernel(const RowsParams p) {
       const int row = 8 * t + 2 * (lane & 3) + (i & 1), group = 2 * cg + (i >> 1);
       if (row < p.M) sums.put(kParts * rank + kh, kCols / 8 * row + group, lane >> 2, acc[t][i]);
     }
-  join_slices<__nv_bfloat16, kCols / 8>(p, reinterpret_cast<const float*>(smem + kStages * kStage), kParts, rank, col0);
+  join_slices<__nv_bfloat16, kCols / 8>(p, reinterpret_cast<const float*>(smem + p.stages * kStage), kParts, rank, col0);
 }
 
 // float32: thread = one column x a part of a stage's steps, MT rows in registers.
@@ -203,7 +204,6 @@ __global__ void __launch_bounds__(kThreads)
 linear_rows_f32_kernel(const RowsParams p) {
   constexpr int kParts = kThreads / kCols, kSteps = kDepth / kParts;
   constexpr int kWBytes = kCols * kDepth * 4, kXBytes = MT * kDepth * 4, kStage = kWBytes + kXBytes;
-  constexpr int kStages = 4;
   pdl_launch_dependents();
   extern __shared__ __align__(1024) uint8_t smem[];
   const int rank = blockIdx.x % p.slices, col0 = (int)(blockIdx.x / p.slices) * kCols;
@@ -219,7 +219,7 @@ linear_rows_f32_kernel(const RowsParams p) {
   constexpr int kWRow = kNK ? kDepth * 4 : kCols * 4;
   auto fetch = [&](int s) {
     const long long k0 = (long long)(first + s) * kDepth;
-    const uint32_t w_dst = smem_at(smem) + (uint32_t)(s % kStages) * kStage, x_dst = w_dst + kWBytes;
+    const uint32_t w_dst = smem_at(smem) + (uint32_t)(s % kStagesF32) * kStage, x_dst = w_dst + kWBytes;
 #pragma unroll
     for (int i = 0; i < kCols * 16 / kThreads; ++i) {
       const int at = threadIdx.x + i * kThreads;
@@ -238,7 +238,7 @@ linear_rows_f32_kernel(const RowsParams p) {
     }
   };
 #pragma unroll
-  for (int s = 0; s < kStages - 1; ++s) {
+  for (int s = 0; s < kStagesF32 - 1; ++s) {
     if (s < count) fetch(s);
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
@@ -248,11 +248,11 @@ linear_rows_f32_kernel(const RowsParams p) {
 #pragma unroll
   for (int m = 0; m < MT; ++m) acc[m] = 0.f;
   for (int s = 0; s < count; ++s) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStagesF32 - 2) : "memory");
     __syncthreads();
-    if (s + kStages - 1 < count) fetch(s + kStages - 1);
+    if (s + kStagesF32 - 1 < count) fetch(s + kStagesF32 - 1);
     asm volatile("cp.async.commit_group;" ::: "memory");
-    const uint8_t* w_src = smem + (s % kStages) * kStage;
+    const uint8_t* w_src = smem + (s % kStagesF32) * kStage;
     const uint8_t* x_src = w_src + kWBytes;
 #pragma unroll
     for (int q = 0; q < kSteps / 4; ++q) {            // four steps at a time
@@ -275,18 +275,18 @@ linear_rows_f32_kernel(const RowsParams p) {
       }
     }
   }
-  const Sums sums(p, kCols / 8, smem_at(smem) + kStages * kStage);
+  const Sums sums(p, kCols / 8, smem_at(smem) + p.stages * kStage);
   cluster_wait();
 #pragma unroll
   for (int m = 0; m < MT; ++m)
     if (m < p.M) sums.put(kParts * rank + kq, kCols / 8 * m + (c >> 3), c & 7, acc[m]);
-  join_slices<float, kCols / 8>(p, reinterpret_cast<const float*>(smem + kStages * kStage), kParts, rank, col0);
+  join_slices<float, kCols / 8>(p, reinterpret_cast<const float*>(smem + p.stages * kStage), kParts, rank, col0);
 }
 
-// dW = x^T dz of up to 64 rows, by fused multiply-adds: a block has 64 rows x 128 columns of dW, a thread 4 x 8 of them, and
-// forms its columns' dz itself; the blocks of the first 64 rows also leave the bias gradient, and dz for the product of dx
-// (they alone, where dW is not wanted).
-// Bound by writing dW, and by the launches that it saves.
+// dW = x^T dz of up to 64 rows, by fused multiply-adds: a block has 128 columns of dW, forms their dz itself, and takes 64 rows
+// of dW after another, a thread 4 x 8 of them; the first block of each 128 columns also leaves the bias gradient, and dz for the
+// product of dx (it alone, where dW is not wanted).  Latency and writing dW bound it: 9 rows, 540 x 372 5 us, 40 rows, 576 x 2752
+// with dropout 11 (the pass over dz and the tensor-core product 6 and 8, and two launches).
 constexpr int kDwRows = 64, kDwCols = 128, kDwPitch = kDwCols + 4;
 template <typename ET>
 __global__ void __launch_bounds__(kThreads)
@@ -300,38 +300,46 @@ linear_rows_dw_kernel(const RowsDw p) {
   const ET* x = static_cast<const ET*>(p.x);
   const ET* dy = static_cast<const ET*>(p.dy);
   const ET* pre = static_cast<const ET*>(p.pre);
-  const long long col0 = (long long)blockIdx.x * kDwCols, k0 = (long long)blockIdx.y * kDwRows;
-  const DropoutState rng = dropout_state(p.dropout);
-  for (int u = threadIdx.x; p.dW != nullptr && u < p.M * (kDwRows / 8); u += kThreads) {
-    const int row = u / (kDwRows / 8), c = u % (kDwRows / 8) * 8;
-    const long long left = p.K - (k0 + c);
-    float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (left > 0) {
-      Raw8<ET> raw;
-      raw.load(x + row * p.ldx + k0 + c, left < 8 ? (int)left : 8);
-      raw.get(f);
-    }
-    store8(xs + row * kDwRows + c, 8, f);
-  }
+  const long long col0 = (long long)blockIdx.x * kDwCols;
   const bool sums = blockIdx.y == 0 && p.dbias != nullptr;
-  for (int u = threadIdx.x; u < p.M * (kDwCols / 8); u += kThreads) {
-    const int row = u / (kDwCols / 8), c = u % (kDwCols / 8) * 8;
-    const long long left = p.N - (col0 + c);
-    float g[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (left > 0) {
-      const int n = left < 8 ? (int)left : 8;
-      Raw8<ET> graw, zraw;
-      float z[8];
-      graw.load(dy + row * p.ldy + col0 + c, n);
-      if (p.act != SWITCH_MOE_ACT_NONE) zraw.load(pre + row * p.ldy + col0 + c, n);
-      graw.get(g);
-      if (p.act != SWITCH_MOE_ACT_NONE) zraw.get(z);
+  // Up to 64 rows of bfloat16 are two groups of eight of x and four of dy and z a thread, 16 of float32 one: all asked for first.
+  constexpr int kX = sizeof(ET) == 2 ? 2 : 1, kG = sizeof(ET) == 2 ? 4 : 1;
+  Raw8<ET> xr[kX], gr[kG], zr[kG];
+  const int x_units = p.dW != nullptr ? p.M * (kDwRows / 8) : 0, g_units = p.M * (kDwCols / 8);
+#pragma unroll
+  for (int i = 0; i < kG; ++i) {
+    const int u = threadIdx.x + i * kThreads, row = u / (kDwCols / 8);
+    const long long col = col0 + u % (kDwCols / 8) * 8, at = row * p.ldy + col;
+    if (u < g_units && col < p.N) {
+      const int n = p.N - col < 8 ? (int)(p.N - col) : 8;
+      gr[i].load(dy + at, n);
+      if (p.act != SWITCH_MOE_ACT_NONE) zr[i].load(pre + at, n);
+    }
+  }
+  auto fetch_x = [&](long long k0) {
+#pragma unroll
+    for (int i = 0; i < kX; ++i) {
+      const int u = threadIdx.x + i * kThreads;
+      const long long k = k0 + u % (kDwRows / 8) * 8;
+      if (u < x_units && k < p.K) xr[i].load(x + u / (kDwRows / 8) * p.ldx + k, p.K - k < 8 ? (int)(p.K - k) : 8);
+    }
+  };
+  fetch_x((long long)blockIdx.y * kDwRows);
+  const DropoutState rng = dropout_state(p.dropout);
+#pragma unroll
+  for (int i = 0; i < kG; ++i) {
+    const int u = threadIdx.x + i * kThreads, row = u / (kDwCols / 8), c = u % (kDwCols / 8) * 8;
+    if (u >= g_units) break;
+    float g[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, z[8];
+    if (col0 + c < p.N) {
+      gr[i].get(g);
+      if (p.act != SWITCH_MOE_ACT_NONE) zr[i].get(z);
       dz8(p.act, p.dropout, rng, (unsigned long long)row * (unsigned)p.per_row + (unsigned)((col0 + c) >> 3), z, g);
       if (p.dz != nullptr && blockIdx.y == 0) store8(static_cast<ET*>(p.dz) + row * p.ldn + col0 + c, 8, g);
     }
     if (sizeof(ET) == 2 && p.round_dz && !sums) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) g[i] = __bfloat162float(__float2bfloat16(g[i]));
+      for (int n = 0; n < 8; ++n) g[n] = __bfloat162float(__float2bfloat16(g[n]));
     }
     store8(gs + row * kDwPitch + c, 8, g);
   }
@@ -352,42 +360,56 @@ linear_rows_dw_kernel(const RowsDw p) {
   }
   if (p.dW == nullptr) return;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;                // columns 8 tx .., rows 4 ty ..
-  float acc[4][8];
+  const long long n = p.N - (col0 + 8 * tx), step = (long long)gridDim.y * kDwRows;
+  for (long long k0 = (long long)blockIdx.y * kDwRows; k0 < p.K; k0 += step) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc[i][j] = 0.f;
-#pragma unroll 2
-  for (int m = 0; m < p.M; ++m) {
-    const float4 a = *reinterpret_cast<const float4*>(xs + m * kDwRows + 4 * ty);
-    float b[8];
-    load8(gs + m * kDwPitch + 8 * tx, 8, b);
-    const float av[4] = {a.x, a.y, a.z, a.w};
+    for (int i = 0; i < kX; ++i) {
+      const int u = threadIdx.x + i * kThreads;
+      float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (u >= x_units) break;
+      if (k0 + u % (kDwRows / 8) * 8 < p.K) xr[i].get(f);
+      store8(xs + u * 8, 8, f);
+    }
+    __syncthreads();
+    if (k0 + step < p.K) fetch_x(k0 + step);
+    float acc[4][8];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[i][j] = fmaf(av[i], b[j], acc[i][j]);
-  }
-  const long long n = p.N - (col0 + 8 * tx);
+      for (int j = 0; j < 8; ++j) acc[i][j] = 0.f;
+#pragma unroll 2
+    for (int m = 0; m < p.M; ++m) {
+      const float4 a = *reinterpret_cast<const float4*>(xs + m * kDwRows + 4 * ty);
+      float b[8];
+      load8(gs + m * kDwPitch + 8 * tx, 8, b);
+      const float av[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const long long k = k0 + 4 * ty + i;
-    if (k < p.K && n > 0) store8(static_cast<ET*>(p.dW) + k * p.ldw + col0 + 8 * tx, n < 8 ? (int)n : 8, acc[i]);
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[i][j] = fmaf(av[i], b[j], acc[i][j]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const long long k = k0 + 4 * ty + i;
+      if (k < p.K && n > 0) store8(static_cast<ET*>(p.dW) + k * p.ldw + col0 + 8 * tx, n < 8 ? (int)n : 8, acc[i]);
+    }
+    __syncthreads();                                   // x's tile has been used by all
   }
 }
 
 template <typename Kern>
-int launch(Kern kernel, size_t smem, int cols, const RowsParams& p, bool* ready, cudaStream_t st) {
+int launch(Kern kernel, size_t stage, int most_stages, size_t sums, int cols, const RowsParams& p, bool* ready, cudaStream_t st) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return SWITCH_MOE_CUDA_ERROR;
   if (dev < 0 || dev >= 64 || !ready[dev]) {
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return SWITCH_MOE_CUDA_ERROR;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(most_stages * stage + sums)) != cudaSuccess)
+      return SWITCH_MOE_CUDA_ERROR;
     if (dev >= 0 && dev < 64) ready[dev] = true;
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(((p.N + (long long)cols - 1) / cols) * p.slices));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = p.stages * stage + sums;      // (with two or three blocks an SM where slices are short)
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -405,16 +427,18 @@ int launch(Kern kernel, size_t smem, int cols, const RowsParams& p, bool* ready,
 constexpr size_t sum_bytes(int parts, int rows, int cols) { return (size_t)parts * (rows * cols / 8 + kMaxSlices) * 32; }
 
 template <bool kNK, int NT, int kCols>
-int launch_bf16(const RowsParams& p, cudaStream_t st) {
+int launch_bf16(RowsParams p, cudaStream_t st) {
   static bool ready[64] = {false};
-  return launch(linear_rows_kernel<kNK, NT, kCols>,
-                (size_t)6 * (kCols * kDepth * 2 + NT * 8 * kDepth * 2) + sum_bytes(8 / (kCols / 16), NT * 8, kCols), kCols, p, ready, st);
+  p.stages = p.depth_per_slice < kStages ? p.depth_per_slice : kStages;
+  return launch(linear_rows_kernel<kNK, NT, kCols>, kCols * kDepth * 2 + NT * 8 * kDepth * 2, kStages,
+                sum_bytes(8 / (kCols / 16), NT * 8, kCols), kCols, p, ready, st);
 }
 template <bool kNK, int MT, int kCols>
-int launch_f32(const RowsParams& p, cudaStream_t st) {
+int launch_f32(RowsParams p, cudaStream_t st) {
   static bool ready[64] = {false};
-  return launch(linear_rows_f32_kernel<kNK, MT, kCols>,
-                (size_t)4 * (kCols * kDepth * 4 + MT * kDepth * 4) + sum_bytes(kThreads / kCols, MT, kCols), kCols, p, ready, st);
+  p.stages = p.depth_per_slice < kStagesF32 ? p.depth_per_slice : kStagesF32;
+  return launch(linear_rows_f32_kernel<kNK, MT, kCols>, kCols * kDepth * 4 + MT * kDepth * 4, kStagesF32,
+                sum_bytes(kThreads / kCols, MT, kCols), kCols, p, ready, st);
 }
 template <bool kNK, int kCols>
 int launch_cols(const DenseProduct& q, const RowsParams& p, cudaStream_t st) {
@@ -464,8 +488,12 @@ int launch_rows_dw(bool f32, const RowsDw& d, cudaStream_t st) {
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess) return SWITCH_MOE_CUDA_ERROR;
     if (dev >= 0 && dev < 64) ready[f32][dev] = true;
   }
-  const long long by = d.dW != nullptr ? ((long long)d.K + kDwRows - 1) / kDwRows : 1;
-  launch_k(kernel, dim3((unsigned)(((long long)d.N + kDwCols - 1) / kDwCols), (unsigned)by), dim3(kThreads), smem, st, d);
+  // about three blocks an SM: more rows of dW per block beyond that
+  const long long bx = ((long long)d.N + kDwCols - 1) / kDwCols, k_tiles = ((long long)d.K + kDwRows - 1) / kDwRows;
+  long long by = 3 * kChipSms / bx;
+  if (by > k_tiles) by = k_tiles;
+  if (by < 1 || d.dW == nullptr) by = 1;
+  launch_k(kernel, dim3((unsigned)bx, (unsigned)by), dim3(kThreads), smem, st, d);
   return launch_status();
 }
 
