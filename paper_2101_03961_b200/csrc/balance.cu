@@ -6,7 +6,8 @@
 // and its number of tokens in the workspace; a second kernel adds the blocks up in a fixed order, 32 experts per block,
 // and the last of its blocks to finish adds up the loss.
 // Backward: one pass, dlogits = p (g - <p, g>), g_i = d_loss alpha E counts_i / (k n^2 groups).
-// Both are bound by reading (and writing) the logits once.
+// Bound by the logits, read (and written) once, and by the instructions on them.  262144 x 128 float32, two choices, eight
+// groups, half of the rows padding (ncu): forward 37 + 6 us, backward 38 us for 67 MB read and 134 written.
 #include <cfloat>
 #include <cmath>
 #include <type_traits>

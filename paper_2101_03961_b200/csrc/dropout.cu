@@ -1,7 +1,8 @@
 // Dropout on its own: y = residual + x keep / (1 - rate), and its backward pass, which is the same without the residual.
 // The mask is drawn from each element's place (dropout_rng.cuh) and never stored, so a call reads its inputs and writes
 // its output once.  A thread takes eight elements of a row: one call of the generator, 16 bytes of bfloat16 or twice 16 of
-// float32 per tensor.
+// float32 per tensor.  32768 x 2048 bfloat16 (ncu): with a residual 64 us, 6.3 TB/s; without one 56, 4.8 TB/s, where the
+// generator's multiplies bound it (93 cycles of a scheduler per warp and eight elements each: 39 us of them).
 #include "dropout_rng.cuh"
 
 namespace swmoe {

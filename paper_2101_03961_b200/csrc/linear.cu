@@ -355,6 +355,8 @@ extern "C" int switch_moe_linear_bwd(const switch_moe_linear_config* cfg, const 
   if (dy == nullptr || (dW != nullptr && x == nullptr) || (dx != nullptr && W == nullptr) ||
       (s.act != SWITCH_MOE_ACT_NONE && pre == nullptr) || (s.q > 0 && rng == nullptr))
     return SWITCH_MOE_INVALID_ARGUMENT;
+  if (dx == nullptr && dW == nullptr && dbias == nullptr)
+    return cudaMemsetAsync(status, 0, kStatusWords * 4, st) == cudaSuccess ? SWITCH_MOE_OK : SWITCH_MOE_CUDA_ERROR;
   if (s.rows_kernel && rows_dw_pays(s.M, s.K, s.N)) {
     // few rows: dW, the bias gradient and, for dx, dz itself in one launch (what is not wanted is left out, so that the rest
     // comes out the same)

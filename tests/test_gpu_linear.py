@@ -196,9 +196,10 @@ def test_float32_products_of_small_and_large_values(scale):
 
 @gpu
 @pytest.mark.parametrize("dtype", [sm.BF16, sm.F32], ids=["bf16", "f32"])
-def test_infinities_and_nan_stay_in_their_rows_and_columns(dtype):
-    c = Case(150, 80, 140, dtype=dtype, act=sm.ACT_RELU)
-    c.x[3, 5], c.x[77, 0], c.W[9, 20], c.x[140, 79] = float("inf"), float("nan"), float("-inf"), 3e38
+@pytest.mark.parametrize("M", [13, 60, 150])
+def test_infinities_and_nan_stay_in_their_rows_and_columns(M, dtype):
+    c = Case(M, 80, 140, dtype=dtype, act=sm.ACT_RELU)
+    c.x[3, 5], c.x[7, 0], c.W[9, 20], c.x[M - 1, 79] = float("inf"), float("nan"), float("-inf"), 3e38
     c.forward()
     x, W, b = c.x.float().cpu(), c.W.float().cpu(), c.bias.float().cpu()
     want = (x.double() @ W.double()).float() + b
@@ -207,14 +208,15 @@ def test_infinities_and_nan_stay_in_their_rows_and_columns(dtype):
     got = c.pre.float().cpu()
     assert torch.equal(torch.isnan(got), torch.isnan(want))
     assert torch.equal(torch.isinf(got), torch.isinf(want.to(got.dtype if dtype == sm.F32 else torch.bfloat16)))
-    assert torch.isnan(c.y[77]).all()                                  # ReLU keeps a NaN
+    assert torch.isnan(c.y[7]).all()                                   # ReLU keeps a NaN
 
 
 @gpu
 @pytest.mark.parametrize("dtype", [sm.BF16, sm.F32], ids=["bf16", "f32"])
-def test_residual_in_place_and_replayed_graph_draws_new_masks(dtype):
+@pytest.mark.parametrize("M", [7, 40, 200])
+def test_residual_in_place_and_replayed_graph_draws_new_masks(M, dtype):
     """y may be the residual; a captured call reads the state when it runs."""
-    c = Case(200, 96, 264, dtype=dtype, residual=True, rate=0.3, act=sm.ACT_GELU)
+    c = Case(M, 96, 264, dtype=dtype, residual=True, rate=0.3, act=sm.ACT_GELU)
     start = c.residual.clone()
     c.forward()
     y0 = c.y.clone()
@@ -271,8 +273,9 @@ def test_gradients_against_differences():
 
 
 @gpu
-def test_optional_outputs_and_empty_calls():
-    c = Case(40, 64, 72, act=sm.ACT_RELU, rate=0.2)
+@pytest.mark.parametrize("M", [40, 300])
+def test_optional_outputs_and_empty_calls(M):
+    c = Case(M, 64, 72, act=sm.ACT_RELU, rate=0.2)
     c.forward()
     c.backward()
     dx, dW, db = c.dx.clone(), c.dW.clone(), c.db.clone()
@@ -283,6 +286,9 @@ def test_optional_outputs_and_empty_calls():
         sm.switch_moe_linear_check_device_status(c.cfg, c.ws)
         for got, full, asked in ((c.dx, dx, want[0]), (c.dW, dW, want[1]), (c.db, db, want[2])):
             assert torch.equal(got, full) if asked else bool((got == 7.0).all())
+    c.ws.fill_(0xFF)                                                   # the status word is written whatever is asked for
+    sm.switch_moe_linear_bwd(c.cfg, c.dy, None, None, c.pre, c.rng, c.ws, None, None, None)
+    sm.switch_moe_linear_check_device_status(c.cfg, c.ws)
     e = Case(0, 64, 72, pad=8)
     e.forward()
     e.backward()
