@@ -248,8 +248,9 @@ balance_rows_kernel(const ET* logits, const int* index, const uint8_t* mask, Bal
       kth = lane_max(below, L);
     }
     uint32_t chosen = 0;
+    const float from = used ? fmaxf(kth, -FLT_MAX) : INFINITY;        // never -infinity; nothing of a row that does not count
 #pragma unroll
-    for (int i = 0; i < V * NV; ++i) chosen |= raw.x[i] >= kth && raw.x[i] != -INFINITY ? 1u << i : 0u;
+    for (int i = 0; i < V * NV; ++i) chosen |= raw.x[i] >= from ? 1u << i : 0u;
     if (!used) chosen = 0;
     if (__any_sync(0xffffffffu, lane_sum(__popc(chosen), L) > s.k)) {
       // ties: the largest logit not yet taken, the lowest index among equals, k times
@@ -375,7 +376,7 @@ balance_sum_kernel(const int* tokens_part, const int* counts_part, const float* 
 }
 
 template <typename ET, int V, int NV>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, V * NV <= 16 ? 4 : 1)
 balance_bwd_kernel(const ET* logits, const uint8_t* mask, const int* counts, const int* tokens, BalanceShape s, int L,
                    float factor, ET* dlogits) {
   pdl_launch_dependents();
