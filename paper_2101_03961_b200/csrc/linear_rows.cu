@@ -82,6 +82,7 @@ __device__ __forceinline__ void prefetch_epilogue(const RowsParams& p, int rank,
 template <typename ET, int kRowGroups>
 __device__ __forceinline__ void join_slices(const RowsParams& p, const float* sums, int sources, int rank, int col0) {
   const DropoutState rng = dropout_state(p.e.dropout);
+  __syncwarp();                                       // (the aligned form wants whole warps)
   cluster_arrive();
   cluster_wait();
   const int groups = (kRowGroups * p.M + p.slices - 1) / p.slices;
@@ -187,6 +188,7 @@ linear_rows_kernel(const RowsParams p) {
     }
   }
   const Sums sums(p, kCols / 8, smem_at(smem) + p.stages * kStage);
+  __syncwarp();
   cluster_wait();                                     // every block of the cluster is there to be written to
 #pragma unroll
   for (int t = 0; t < NT; ++t)
@@ -276,6 +278,7 @@ linear_rows_f32_kernel(const RowsParams p) {
     }
   }
   const Sums sums(p, kCols / 8, smem_at(smem) + p.stages * kStage);
+  __syncwarp();
   cluster_wait();
 #pragma unroll
   for (int m = 0; m < MT; ++m)
