@@ -5,7 +5,7 @@
 // sum of its probabilities stay in registers.  A block works on rows of one group and leaves its sums P, its integer counts
 // and its number of tokens in the workspace; a second kernel adds the blocks up in a fixed order, 32 experts per block,
 // and the last of its blocks to finish adds up the loss.
-// Backward: one pass, dlogits = p (g - <p, g>), g_i = d_loss alpha E counts_i / (k n^2 groups).
+// Backward: one pass, dlogits = p (g - <p, g>), g_i = d_loss alpha E (counts_i - counts_0) / (k n^2 groups).
 // Bound by the logits, read (and written) once, and by the instructions on them.  262144 x 128 float32, two choices, eight
 // groups, half of the rows padding (ncu): forward 37 + 6 us, backward 38 us for 67 MB read and 134 written.
 #include <cfloat>
@@ -386,11 +386,14 @@ balance_bwd_kernel(const ET* logits, const uint8_t* mask, const int* counts, con
   const long long row0 = (long long)g * s.Tg;
   const int n = tokens[g];
   const float up = n > 0 ? factor / ((float)n * (float)n) : 0.f;   // factor = d_loss alpha E / (k groups)
+  // p (g - <p, g>) does not change with a constant added to g, as the probabilities sum to one: counted from the first
+  // expert's choices, the more even the router, the less cancels (and nothing is left where all are chosen alike).
+  const int base = counts[(long long)g * s.E];
   float grad[V * NV];
 #pragma unroll
   for (int i = 0; i < V * NV; ++i) {
     const int e = (l + (i / V) * L) * V + i % V;
-    grad[i] = e < s.E ? up * (float)counts[(long long)g * s.E + e] : 0.f;
+    grad[i] = e < s.E ? up * (float)(counts[(long long)g * s.E + e] - base) : 0.f;
   }
   const int stride = (int)gridDim.x * kWarps * per_warp;
   const int first = ((int)blockIdx.x * kWarps + warp) * per_warp;

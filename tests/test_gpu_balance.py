@@ -166,6 +166,15 @@ def test_gradient_against_differences():
 
 
 @gpu
+@pytest.mark.parametrize("E,dtype", [(2, sm.F32), (4, sm.BF16), (9, sm.F32)])
+def test_every_expert_chosen_leaves_no_gradient(E, dtype):
+    """k = E: f is 1 / E for every expert, the loss alpha whatever the router does."""
+    loss, counts, tokens, dl = call(randn(300, E, dtype=dtype), k=E, groups=3, dtype=dtype)
+    assert bool((counts == 100).all()) and not dl.any()
+    assert abs(float(loss) - 0.01) <= 0.01 * (2.0**-19 + 24 * 2.0**-24)
+
+
+@gpu
 def test_the_layer_and_this_loss_agree():
     """The layer's own auxiliary loss, from the probabilities' logits and its expert indices."""
     from paper_2101_03961_b200 import inputs as si
