@@ -1,12 +1,14 @@
 // The dense product of few rows (a decoding step): out = x W with the whole epilogue, or dx = dz W^T, up to 64 rows of
-// bfloat16 or 16 of float32 (fused multiply-adds: 31 rows, 1792 x 8064 took 101 us here, 50 as bfloat16 parts on the tensor cores).  Such a call reads W once and little else, so it is all latency and bandwidth: a tile of the
-// tensor-core kernel (256 rows, one CTA pair per 128 columns and all of the contraction) would leave most SMs without work.
+// bfloat16 or 16 of float32 (fused multiply-adds: 31 rows, 1792 x 8064 took 101 us here, 50 as bfloat16 parts on the tensor
+// cores).  Such a call reads W once and little else, so it is all latency and bandwidth: a tile of the tensor-core kernel
+// (256 rows, one CTA pair per 128 columns and all of the contraction) would leave most SMs without work.
 //
-// Here a block has 64 output columns (32 where that leaves SMs without a block) and a slice of the contraction; the blocks of the other slices form a cluster with it.
-// The groups of eight outputs are dealt out to the cluster's blocks; each block writes its sums into the shared memory
-// of the one that finishes them, and after one cluster barrier that one adds them up in a fixed order.  64-deep pieces of W and x come in by cp.async,
-// up to kStages at a time.  bfloat16: warp-level MMAs (16 columns of W x 8 rows of x x 16 steps: with so few rows a
-// tcgen05 tile would be padding, and the loads bound it in either case); float32: fused multiply-adds.
+// Here a block has 64 output columns (32 where that leaves SMs without a block) and a slice of the contraction; the blocks
+// of the other slices form a cluster with it.  The groups of eight outputs are dealt out to the cluster's blocks; each block
+// writes its sums into the shared memory of the one that finishes them, and after one cluster barrier that one adds them up
+// in a fixed order.  64-deep pieces of W and x come in by cp.async, up to kStages at a time.  bfloat16: warp-level MMAs
+// (16 columns of W x 8 rows of x x 16 steps: with so few rows a tcgen05 tile would be padding, and the loads bound it in
+// either case); float32: fused multiply-adds.
 // One token, 768 x 2048, GELU: 6.0 us serialised by ncu for 3.1 MB of weights (the tile kernel 11), 48 rows, 2048 x 768 9 (14).
 #include "linear_common.cuh"
 
