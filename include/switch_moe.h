@@ -316,7 +316,9 @@ int switch_moe_stage_launches(const switch_moe_config* cfg, int32_t* launches_ou
  * of a model apart that share a state.  The rates lie in [0, 1); a rate whose q is 65536 is refused, one whose q is 0
  * drops nothing. */
 
-enum switch_moe_activation { SWITCH_MOE_ACT_NONE = 0, SWITCH_MOE_ACT_RELU = 1, SWITCH_MOE_ACT_GELU = 2 /* z Phi(z) */ };
+/* GELU: z Phi(z).  Phi(-|z|) has a relative error below 1e-6 up to |z| = 2, 6e-6 up to 6 and 8e-5 up to 10; from there on GELU's
+ * negative side and its derivative's are a constant below 1e-21. */
+enum switch_moe_activation { SWITCH_MOE_ACT_NONE = 0, SWITCH_MOE_ACT_RELU = 1, SWITCH_MOE_ACT_GELU = 2 };
 
 /* Dense product with its epilogue, the FFN and projections of the layers between Switch layers:
  *   z = x W + bias,   y = residual + dropout(activation(z)). */

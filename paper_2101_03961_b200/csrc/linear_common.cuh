@@ -94,57 +94,52 @@ __device__ __forceinline__ uint64_t pair_add(uint64_t a, uint64_t b) {
   return r;
 }
 
-// GELU and its derivative, two values at a time and without selections: with a = min(|z|, 6), beyond which Phi(-a) and
-// a phi(a) are below 4e-8, and q = -Phi(-a),
-//   GELU(z) = max(z, 0) + a q,   GELU'(z) = 1/2 + sign(z) (1/2 + q + a phi(a)).
-// q = P(a) exp(-a^2 / 2) with a polynomial of degree 10 fitted to -Phi(-a) exp(a^2 / 2) on [0, 6], least in the largest error
-// that it makes in q and in a q: 1.5e-7 both, float32 evaluation included (the rational form of gelu_cdf_pdf: 7.5e-8 in q, 4e-7
-// in a q).  Packed, a value costs 10 issue slots and one special function; the rational form's reciprocal makes it two of
-// those, whose unit takes a quarter of a warp a cycle.  min and max keep a NaN.
-__device__ __forceinline__ float min_nan(float a, float b) {
-  float r;
-  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
+// GELU and its derivative, two values at a time: with n = max(-|z|, -10),
+//   GELU(z) = max(z, 0) + n Phi(n),   GELU'(z) = Phi(n) + n phi(n), or 1 minus that for z > 0.
+// Phi(n) = 2^R(n) with a polynomial R of degree 12 fitted to log2 Phi on [-10, 0], so that the tail keeps its relative error:
+// float32 evaluation included 7.3e-7 from -2 on, 5.2e-6 from -6 on, 7.5e-5 from -10 on, and 3.6e-8 absolute in n Phi(n).  Below -10
+// GELU is the constant -7.6e-23.  A form with an absolute error, P(a) exp(-a^2 / 2), is off by 8% at -5 and needs as many
+// instructions; erfc, or a rational form with its reciprocal, needs a second special function a value, whose unit takes a quarter
+// of a warp a cycle.  min and max keep a NaN.
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
 __device__ __forceinline__ uint64_t pair_same(float v) { return pair_of(v, v); }
-// q's factors P(a) and exp(-a^2 / 2).
-__device__ __forceinline__ void gelu_tail(uint64_t a, uint64_t* poly, uint64_t* e) {
-  const float2 x = halves_of(pair_mul(pair_mul(a, pair_same(-0.72134752044448170f)), a));
-  float2 ex;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(ex.x) : "f"(x.x));
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(ex.y) : "f"(x.y));
-  *e = pair_of(ex.x, ex.y);
-  uint64_t s = pair_fma(pair_same(-1.2713327350866166e-06f), a, pair_same(2.8995684260735288e-05f));
-  s = pair_fma(s, a, pair_same(-0.000295169185847044f));
-  s = pair_fma(s, a, pair_same(0.0018014268716797233f));
-  s = pair_fma(s, a, pair_same(-0.007541901897639036f));
-  s = pair_fma(s, a, pair_same(0.02376292459666729f));
-  s = pair_fma(s, a, pair_same(-0.06070178374648094f));
-  s = pair_fma(s, a, pair_same(0.1323055922985077f));
-  s = pair_fma(s, a, pair_same(-0.24986957013607025f));
-  s = pair_fma(s, a, pair_same(0.39893248677253723f));
-  *poly = pair_fma(s, a, pair_same(-0.49999988079071045f));
+__device__ __forceinline__ uint64_t pair_exp2(uint64_t v) {
+  const float2 x = halves_of(v);
+  float2 e;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(x.x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(x.y));
+  return pair_of(e.x, e.y);
+}
+__device__ __forceinline__ uint64_t normal_tail(uint64_t n) {          // Phi(n)
+  uint64_t r = pair_fma(pair_same(-4.2411133632791476e-11f), n, pair_same(-2.6161950383851718e-09f));
+  r = pair_fma(r, n, pair_same(-7.09738188220399e-08f));
+  r = pair_fma(r, n, pair_same(-1.1100130450358847e-06f));
+  r = pair_fma(r, n, pair_same(-1.0956950063700788e-05f));
+  r = pair_fma(r, n, pair_same(-6.879954162286595e-05f));
+  r = pair_fma(r, n, pair_same(-0.00023773251450620592f));
+  r = pair_fma(r, n, pair_same(0.0001084727919078432f));
+  r = pair_fma(r, n, pair_same(0.007098168600350618f));
+  r = pair_fma(r, n, pair_same(0.05255275219678879f));
+  r = pair_fma(r, n, pair_same(-0.45918235182762146f));
+  r = pair_fma(r, n, pair_same(1.1511086225509644f));
+  return pair_exp2(pair_fma(r, n, pair_same(-1.f)));
 }
 __device__ __forceinline__ void gelu_pair(float* z0, float* z1) {
-  const uint64_t a = pair_of(min_nan(fabsf(*z0), 6.f), min_nan(fabsf(*z1), 6.f));
-  uint64_t poly, e;
-  gelu_tail(a, &poly, &e);
-  const float2 r = halves_of(pair_fma(a, pair_mul(poly, e), pair_of(max_nan(*z0, 0.f), max_nan(*z1, 0.f))));
+  const uint64_t n = pair_of(max_nan(-fabsf(*z0), -10.f), max_nan(-fabsf(*z1), -10.f));
+  const float2 r = halves_of(pair_fma(n, normal_tail(n), pair_of(max_nan(*z0, 0.f), max_nan(*z1, 0.f))));
   *z0 = r.x;
   *z1 = r.y;
 }
 __device__ __forceinline__ float2 gelu_grad_pair(float z0, float z1) {
-  const uint64_t a = pair_of(min_nan(fabsf(z0), 6.f), min_nan(fabsf(z1), 6.f));
-  uint64_t poly, e;
-  gelu_tail(a, &poly, &e);
-  // 1/2 + e (poly + a / sqrt(2 pi))
-  const float2 h = halves_of(pair_fma(e, pair_fma(a, pair_same(0.3989422804014327f), poly), pair_same(0.5f)));
-  return halves_of(pair_add(pair_of(copysignf(h.x, z0), copysignf(h.y, z1)), pair_same(0.5f)));
+  const uint64_t n = pair_of(max_nan(-fabsf(z0), -10.f), max_nan(-fabsf(z1), -10.f));
+  // phi(n) = 2^(-n^2 / 2 log2 e - log2 sqrt(2 pi))
+  const uint64_t density = pair_exp2(pair_fma(pair_mul(n, n), pair_same(-0.72134752044448170f), pair_same(-1.3257480647361593f)));
+  const float2 w = halves_of(pair_fma(n, density, normal_tail(n)));
+  return make_float2(z0 > 0.f ? 1.f - w.x : w.x, z1 > 0.f ? 1.f - w.y : w.y);
 }
 
 // Everything after the product for eight results of a row: bias, z saved, activation, dropout, residual, store.
