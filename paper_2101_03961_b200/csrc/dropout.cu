@@ -69,14 +69,14 @@ dropout_kernel(const ET* x, const ET* res, ET* y, long long blocks, int per_row,
   pdl_wait();
   constexpr int kAhead = 2;
   const DropoutState s = dropout_state(d);
-  const long long step = (long long)gridDim.x * kThreads * kAhead;
-  for (long long b0 = (long long)blockIdx.x * kThreads * kAhead + threadIdx.x; b0 < blocks; b0 += step) {
+  const long long step = (long long)gridDim.x * kThreads;   // a thread's two are a grid apart: a small call has one, in every block
+  for (long long b0 = (long long)blockIdx.x * kThreads + threadIdx.x; b0 < blocks; b0 += kAhead * step) {
     Eight<ET> a[kAhead], r[kAhead];
     long long at[kAhead];
     int n[kAhead];                                    // elements of the block that are in the row
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      const long long b = b0 + k * kThreads;
+      const long long b = b0 + k * step;
       n[k] = 0;
       if (b >= blocks) continue;
       if (kDense) {
@@ -98,7 +98,7 @@ dropout_kernel(const ET* x, const ET* res, ET* y, long long blocks, int per_row,
     }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      const long long b = b0 + k * kThreads;
+      const long long b = b0 + k * step;
       if (b >= blocks) break;
       float v[8];
       a[k].get(v);
