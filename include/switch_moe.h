@@ -339,7 +339,8 @@ typedef struct switch_moe_linear_config {
 int switch_moe_linear_workspace_bytes(const switch_moe_linear_config* cfg, int32_t backward, size_t* bytes_out);
 
 /* Forward.  x [M,K]; W [K,N]; bias float32[N] or NULL; residual [M,N] or NULL (may be y itself); rng: see above;
- * y [M,N] (out); pre [M,N] (out) receives z for the backward pass, or NULL.  x, W and bias may not overlap y or pre.
+ * y [M,N] (out); pre [M,N] (out) receives z for the backward pass, or NULL.  x, W and bias may not overlap y or pre;
+ * pre may not overlap y or residual (INVALID_ARGUMENT where it is one of them).
  * bf16: products on the tensor cores, float32 sums; f32: the same cores on sums of exact bfloat16 parts, error against
  * float64 like float32 FMA's (a result that is not finite, or from 2^80 on, is formed by FMA); up to 64 rows
  * of bf16 or 16 of f32 a kernel that splits the contraction instead of the rows, f32 by FMA. */

@@ -315,6 +315,7 @@ extern "C" int switch_moe_linear_fwd(const switch_moe_linear_config* cfg, const 
   if (!aligned16(x) || !aligned16(W) || !aligned16(y) || !aligned16(pre) || !aligned16(residual) || !aligned16(bias) ||
       (reinterpret_cast<uintptr_t>(rng) & 7u) != 0)
     return SWITCH_MOE_UNSUPPORTED_SHAPE;
+  if (pre != nullptr && (pre == y || pre == residual)) return SWITCH_MOE_INVALID_ARGUMENT;   // z would meet y, or replace what is added
   DenseProduct q{};
   q.rows = s.M; q.cols = s.N; q.k = s.K; q.f32 = s.f32;
   q.a = {x, s.ldx, static_cast<const float*>(x), s.ldx, 1};

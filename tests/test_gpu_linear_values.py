@@ -74,3 +74,15 @@ def test_gelu_and_its_derivative_keep_their_tails(M, K, dtype):
     bound = tail * phi_error(a) + slope * density_error(a.clamp(max=100.0)) + 2.0**-23 * want.abs() + 2.0**-24 * w.abs() + 10 * lost
     bad = ~((db.cpu().double() - want).abs() <= bound)
     assert not bad.any(), (int(bad.sum()), z[bad][:4], db.cpu()[bad][:4], want[bad][:4])
+
+
+def test_saved_pre_activations_on_top_of_the_output_or_the_residual_are_refused():
+    """Both are written, or read, in the same pass: z would take y's place or be added as the residual."""
+    sbuild.build()
+    lib = sm.load_library()
+    cfg = sm.make_linear_config(32, 64, 72, activation=sm.ACT_GELU)
+    n = sm.switch_moe_linear_workspace_bytes(cfg)
+    call = lambda res, y, pre: lib.switch_moe_linear_fwd(cfg, 16, 32, None, res, None, y, pre, 1024, n, None)
+    assert call(None, 48, 48) == sm.INVALID_ARGUMENT
+    assert call(64, 48, 64) == sm.INVALID_ARGUMENT
+    assert call(48, 48, 48) == sm.INVALID_ARGUMENT
