@@ -352,7 +352,9 @@ int switch_moe_linear_fwd(const switch_moe_linear_config* cfg, const void* x, co
  *   dz = dropout(dy) . activation'(pre),  dx = dz W^T,  dW = x^T dz,  dbias = sum of dz over rows;
  * the residual's gradient is dy itself.  pre: what the forward call wrote (for RELU any tensor with the same signs, such
  * as y without dropout and residual); NULL only for ACT_NONE.  Each of dx, dW, dbias may be NULL: not wanted.  x may be
- * NULL without dW, W without dx.  No output may overlap an input.  bf16: dx and dW are products of dz rounded to bfloat16, dbias sums it unrounded.
+ * NULL without dW, W without dx.  No output may overlap an input.  bf16: dx and dW are products of dz rounded to bfloat16 (where activation
+ * or dropout form one; dW of up to 64 rows, where it is small, takes it in float32), dbias sums it unrounded; z itself is what pre
+ * holds, rounded.
  * M = 0 writes zeros to dW and dbias. */
 int switch_moe_linear_bwd(const switch_moe_linear_config* cfg, const void* dy, const void* x, const void* W,
                           const void* pre, const uint64_t* rng, void* workspace, size_t workspace_bytes, void* dx,

@@ -53,7 +53,6 @@ struct RowsDw {
   void* dW; float* dbias; void* dz;
   int M, K, N, act, per_row;
   long long ldx, ldw, ldy, ldn;
-  bool round_dz;                   // dz is rounded to the activation type before it is multiplied
   DropoutParams dropout;
   int* status;
 };

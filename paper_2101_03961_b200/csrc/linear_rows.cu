@@ -290,7 +290,7 @@ linear_rows_f32_kernel(const RowsParams p) {
 
 // dW = x^T dz of up to 64 rows, by fused multiply-adds: a block has 128 columns of dW, forms their dz itself, and takes 64 rows
 // of dW after another, a thread 4 x 8 of them; the first block of each 128 columns also leaves the bias gradient, and dz for the
-// product of dx (it alone, where dW is not wanted).  Latency and writing dW bound it: 9 rows, 540 x 372 5 us, 40 rows, 576 x 2752
+// product of dx (it alone, where dW is not wanted).  dW takes dz in float32, as it was formed; dx's tensor cores take it rounded.  Latency and writing dW bound it: 9 rows, 540 x 372 5 us, 40 rows, 576 x 2752
 // with dropout 11 (the pass over dz and the tensor-core product 6 and 8, and two launches).
 constexpr int kDwRows = 64, kDwCols = 128, kDwPitch = kDwCols + 4;
 template <typename ET>
@@ -342,26 +342,13 @@ linear_rows_dw_kernel(const RowsDw p) {
       dz8(p.act, p.dropout, rng, (unsigned long long)row * (unsigned)p.per_row + (unsigned)((col0 + c) >> 3), z, g);
       if (p.dz != nullptr && blockIdx.y == 0) store8(static_cast<ET*>(p.dz) + row * p.ldn + col0 + c, 8, g);
     }
-    if (sizeof(ET) == 2 && p.round_dz && !sums) {
-#pragma unroll
-      for (int n = 0; n < 8; ++n) g[n] = __bfloat162float(__float2bfloat16(g[n]));
-    }
     store8(gs + row * kDwPitch + c, 8, g);
   }
   __syncthreads();
-  if (sums) {                                          // of dz as it is, before it is rounded
-    if (threadIdx.x < kDwCols && col0 + threadIdx.x < p.N) {
-      float s = 0.f;
-      for (int m = 0; m < p.M; ++m) s += gs[m * kDwPitch + threadIdx.x];
-      p.dbias[col0 + threadIdx.x] = s;
-    }
-    __syncthreads();
-    if (sizeof(ET) == 2 && p.round_dz)
-      for (int u = threadIdx.x; u < p.M * kDwCols; u += kThreads) {
-        float* at = gs + u / kDwCols * kDwPitch + u % kDwCols;
-        *at = __bfloat162float(__float2bfloat16(*at));
-      }
-    __syncthreads();
+  if (sums && threadIdx.x < kDwCols && col0 + threadIdx.x < p.N) {
+    float s = 0.f;
+    for (int m = 0; m < p.M; ++m) s += gs[m * kDwPitch + threadIdx.x];
+    p.dbias[col0 + threadIdx.x] = s;
   }
   if (p.dW == nullptr) return;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;                // columns 8 tx .., rows 4 ty ..

@@ -86,3 +86,28 @@ def test_saved_pre_activations_on_top_of_the_output_or_the_residual_are_refused(
     assert call(None, 48, 48) == sm.INVALID_ARGUMENT
     assert call(64, 48, 64) == sm.INVALID_ARGUMENT
     assert call(48, 48, 48) == sm.INVALID_ARGUMENT
+
+
+@gpu
+@pytest.mark.parametrize("act,rate", [(sm.ACT_GELU, 0.0), (sm.ACT_NONE, 0.3), (sm.ACT_GELU, 0.3)], ids=["gelu", "drop", "gelu_drop"])
+@pytest.mark.parametrize("M", [1, 2, 9, 40, 64])
+def test_weight_gradient_of_few_rows_takes_dz_unrounded(M, act, rate):
+    """bfloat16, the kernel that forms dz itself and multiplies it in float32: one rounding of each result, none of dz."""
+    sbuild.build()
+    K, N, key = 72, 200, 1234567
+    g = torch.Generator(device="cuda").manual_seed(M)
+    x, W, dy, z = (torch.randn(*s, device="cuda", generator=g).bfloat16() for s in ((M, K), (K, N), (M, N), (M, N)))
+    dW, db = torch.empty_like(W), torch.empty(N, device="cuda")
+    rng = torch.tensor([key, 3], device="cuda")
+    cfg = sm.make_linear_config(M, K, N, activation=act, dropout=rate, site=4)
+    ws = sm.allocate_linear_workspace(cfg, backward=True)
+    sm.switch_moe_linear_bwd(cfg, dy, x, W, z, rng, ws, None, dW, db)
+    sm.switch_moe_linear_check_device_status(cfg, ws)
+    dz = ref.to64(dy) * ref.dropout_factors(M, N, rate, 4, key, 3) * ref.d_act(ref.to64(z), act)
+    xs = ref.to64(x)
+    want, size = xs.T @ dz, abs(xs).T @ abs(dz)
+    # dz: the mask's scale and product 2^-23, GELU' 1e-6 of its terms (up to 0.5 each) and one product; sums of M products
+    slope = 1e-6 * (abs(xs).T @ abs(ref.to64(dy))) / (1 - rate) if act else 0.0
+    bound = 2.0**-8 * abs(want) + 1.01 * ((M + 4) * 2.0**-23 * size + slope)
+    bad = abs(ref.to64(dW) - want) > bound
+    assert not bad.any(), (int(bad.sum()), bad.size)
