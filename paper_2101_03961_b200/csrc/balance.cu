@@ -6,8 +6,11 @@
 // and its number of tokens in the workspace; a second kernel adds the blocks up in a fixed order, 32 experts per block,
 // and the last of its blocks to finish adds up the loss.
 // Backward: one pass, dlogits = p (g - <p, g>), g_i = d_loss alpha E (counts_i - counts_0) / (k n^2 groups).
-// Bound by the logits, read (and written) once, and by the instructions on them.  262144 x 128 float32, two choices, eight
-// groups, half of the rows padding (ncu): forward 35 + 6.5 us, backward 36 us for 67 MB read and 134 written.
+// Bound by the logits, read (and written) once, and by the instructions on them (0.6 a cycle and scheduler at two blocks an SM).
+// 262144 x 128 float32, two choices, eight groups (ncu): forward 48 + 6 us, and with half of the rows padding 34 where every group
+// has as many, 46 where they have 1/9 to 8/9: a group's blocks work on its rows alone, so that the launch lasts as long as the
+// group with the most tokens.  Backward, which writes every row, 36 us with two thirds of the rows padding; four blocks an SM
+// there cost one layout (float32, four pieces a lane) 16 bytes of spills.
 #include <cfloat>
 #include <cmath>
 #include <type_traits>

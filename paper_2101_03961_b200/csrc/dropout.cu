@@ -1,8 +1,9 @@
 // Dropout on its own: y = residual + x keep / (1 - rate), and its backward pass, which is the same without the residual.
 // The mask is drawn from each element's place (dropout_rng.cuh) and never stored, so a call reads its inputs and writes
 // its output once.  A thread takes eight elements of a row: one call of the generator, 16 bytes of bfloat16 or twice 16 of
-// float32 per tensor.  32768 x 2048 bfloat16 (ncu): with a residual 64 us, 6.3 TB/s; without one 56, 4.8 TB/s, where the
-// generator's multiplies bound it (93 cycles of a scheduler per warp and eight elements each: 39 us of them).
+// float32 per tensor.  32768 x 2048 bfloat16 (ncu): with a residual 64 us, 6.3 TB/s; without one 53, 5.1 TB/s.  There neither the
+// bytes (41 us) nor the generator's multiplies (93 cycles of a scheduler per warp and eight elements each, 21 us) bound it alone:
+// 0.6 instructions a cycle and scheduler with two loads of 16 bytes in flight a thread.
 #include "dropout_rng.cuh"
 
 namespace swmoe {
@@ -61,7 +62,8 @@ template <> struct Eight<float> {
 };
 
 // kDense: rows follow each other without a gap and in whole blocks of eight.  Two blocks of eight per thread are asked for
-// before the first is worked on: with one, the loads' latency bounded the kernel (0.6 instructions a cycle and scheduler).
+// before the first is worked on; with one, the loads' latency bounded the kernel.  Five and four blocks an SM; float32 with a
+// residual spills 20 bytes for it (rows with gaps 76).
 template <typename ET, bool kRes, bool kDense>
 __global__ void __launch_bounds__(kThreads, sizeof(ET) == 2 ? 5 : 4)
 dropout_kernel(const ET* x, const ET* res, ET* y, long long blocks, int per_row, int cols, long long ld, DropoutParams d) {

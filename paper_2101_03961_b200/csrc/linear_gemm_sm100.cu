@@ -8,14 +8,16 @@
 // and works on its own: 32 columns at a time from tensor memory through the epilogue into 64-byte-swizzled shared memory,
 // and from there by TMA, which also brings the residual into the very buffer that the result leaves from and clips what is
 // outside (a store in whole 16-byte pieces: the last columns of a row that does not end on one are written element by
-// element).  With GELU the epilogue is latency-bound (ncu: 0.30 instructions a cycle and scheduler with eight warps), hence
-// sixteen.
+// element).  With GELU the epilogue is bound by latency (32768 x 768 x 2048, z saved: eight warps 169 us, sixteen 120, at 0.5
+// instructions a cycle and scheduler), hence sixteen.
 //
+// Sums of bfloat16 products stay in the tensor pipe over the whole contraction, which truncates each addition to float32: 2^-23
+// a step of 16, far below the result's rounding unless thousands of steps cancel.
 // Float32 operands come as three bfloat16 parts (x 2^24 = h + m + l, exact); of the nine cross products six are formed,
 // the others are below 2^-25 of the product.  The tensor pipe adds with truncation, so an accumulator lives for one block
 // of 64 steps only (the corrections first, h.h last) and is then added to a float32 sum in registers, round to nearest.
 // Results that are not finite are formed again by fused multiply-adds from the float32 operands (operands from 2^104 on
-// and sums from 2^80 on end there too).
+// and sums from 2^80 on end there too).  Its wide tiles hold up to 64 sums a thread and spill 88 (192 columns) to 144 bytes.
 //
 // Every wait is bounded in time; after one gave up all roles leave.
 #include <algorithm>
@@ -281,7 +283,7 @@ dense_gemm_kernel(const __grid_constant__ DenseMaps maps, const __grid_constant_
           } else {
             // Six of the nine part products; a part is loaded once and released after its last: the low one after half of
             // the block, so that the next block's is there in time.  (Loaded anew for every product, 24 or 32 KB per 256
-            // or 512 cycles of the tensor pipe, L2 bounded it: 54% tensor activity.)
+            // or 512 cycles of the tensor pipe, they took longer: 4001 tokens, 512 x 2048, GELU, a training step 234 us, so 205.)
             uint32_t s[3], ph[3];
 #pragma unroll
             for (int i = 0; i < 3; ++i) {
@@ -689,10 +691,10 @@ int launch_kind(const DenseProduct& q, const DenseEpilogue& e, cudaStream_t st) 
 }  // namespace
 
 // The tiling whose estimated time is least.  A round of tiles over the CTA pairs takes a time per 64 steps of the contraction
-// that falls with the width, but by less than the width does, since A is staged as before (us with 256 / 192 / 128 columns:
-// 32768 tokens, 2048 x 768 forward 78 / 82 / 88, dx of 768 x 2048, k-major, 87 / 81 / 94; 8192 tokens, 768 x 2048 22.4 / 24.2 /
-// 25.3; 1000 tokens 10.2 / 9.6 / 8.1; float32 4001, 512 x 2048 forward 51 / 58 / 50, dx 84 / 72 / 56), and one for its
-// epilogue.  Cutting the contraction fills the pairs where the output has few tiles, a weight gradient's or that of a few
+// that falls with the width, but by less than the width does, since A is staged as before (us with 256 / 192 / 128 columns,
+// the kernel alone after cold caches, ncu: 32768 tokens, 2048 x 768 forward 75.6 / 75.6 / 103, dx of 768 x 2048, k-major, 75.8 / 72.7 /
+// 82.6; 8192 tokens, 768 x 2048 25.9 / 27.2 / 32.5; 1000 tokens 11.9 / 10.7 / 10.7; float32 4001, 512 x 2048 forward 47.6 / 52.7 /
+// 45.2, where the rule takes 256, dx 43.0 / 45.2 / 41.2), and one for its epilogue.  Cutting the contraction fills the pairs where the output has few tiles, a weight gradient's or that of a few
 // hundred tokens; the parts are written and read once more, by one more launch.
 DenseTiling dense_tiling(DenseKind kind, bool f32, long long rows, long long cols, long long k) {
   const long long pairs = kChipSms / 2, m = (rows + 255) / 256, blocks = (k + kBK - 1) / kBK;

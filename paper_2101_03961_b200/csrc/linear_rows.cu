@@ -9,7 +9,8 @@
 // in a fixed order.  64-deep pieces of W and x come in by cp.async, up to kStages at a time.  bfloat16: warp-level MMAs
 // (16 columns of W x 8 rows of x x 16 steps: with so few rows a tcgen05 tile would be padding, and the loads bound it in
 // either case); float32: fused multiply-adds.
-// One token, 768 x 2048, GELU: 6.0 us serialised by ncu for 3.1 MB of weights (the tile kernel 11), 48 rows, 2048 x 768 9 (14).
+// One token, 768 x 2048, GELU: 6.0 us serialised by ncu for 3.1 MB of weights (the tile kernel 11), 48 rows, 2048 x 768 9.9 (14): there
+// 32 sums (8 slices of 4 parts of the steps) meet in each output, added up by 24 threads a block.
 #include "linear_common.cuh"
 
 namespace swmoe {
@@ -290,8 +291,9 @@ linear_rows_f32_kernel(const RowsParams p) {
 
 // dW = x^T dz of up to 64 rows, by fused multiply-adds: a block has 128 columns of dW, forms their dz itself, and takes 64 rows
 // of dW after another, a thread 4 x 8 of them; the first block of each 128 columns also leaves the bias gradient, and dz for the
-// product of dx (it alone, where dW is not wanted).  dW takes dz in float32, as it was formed; dx's tensor cores take it rounded.  Latency and writing dW bound it: 9 rows, 540 x 372 5 us, 40 rows, 576 x 2752
-// with dropout 11 (the pass over dz and the tensor-core product 6 and 8, and two launches).
+// product of dx (it alone, where dW is not wanted).  dW takes dz in float32, as it was formed; dx's tensor cores take it rounded.
+// Latency and writing dW bound it (GELU): 9 rows, 540 x 372 5.6 us, 16 rows, 512 x 2880 7, where the pass over dz and the
+// tensor-core product take two launches of 6 to 8.
 constexpr int kDwRows = 64, kDwCols = 128, kDwPitch = kDwCols + 4;
 template <typename ET>
 __global__ void __launch_bounds__(kThreads)
