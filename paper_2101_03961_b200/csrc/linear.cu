@@ -107,8 +107,9 @@ __device__ __forceinline__ void store_parts8(__nv_bfloat16* p, long long plane, 
 // double both products; dx's and dW's error against float64 is 0.0023 of the norm for 0.0017 with dz in float32); the column sums
 // take it unrounded.  A block takes 256 columns of a chunk of rows: 32 threads x 8 columns, 8 rows side by side; a
 // thread asks for two of its rows before it works on the first (32768 x 2048, GELU: 83 us; with a GELU' of 5 us less four rows
-// ahead and three blocks an SM took 82, two ahead and five blocks 91, against 78).  Column sums go to `part`, from where they are added up in chunk order.  Bound by reading
-// dy and pre and writing dz once (ReLU 16384 x 10240: 148 us, 6.8 TB/s); with GELU and dropout by instructions.
+// ahead and three blocks an SM took 82, two ahead and five blocks 91, against 78).  Column sums go to `part`, from where they are
+// added up in chunk order.  Bound by reading dy and pre and writing dz once (ReLU 16384 x 10240: 148 us, 6.8 TB/s); with GELU and
+// dropout by instructions.
 struct DzArgs {
   int M, N, act, chunk_rows, per_row;
   long long ldy, ldn;

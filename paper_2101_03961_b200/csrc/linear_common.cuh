@@ -87,11 +87,6 @@ __device__ __forceinline__ uint64_t pair_mul(uint64_t a, uint64_t b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
-__device__ __forceinline__ uint64_t pair_add(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
 
 // GELU and its derivative, two values at a time: with n = max(-|z|, -10),
 //   GELU(z) = max(z, 0) + n Phi(n),   GELU'(z) = Phi(n) + n phi(n), or 1 minus that for z > 0.

@@ -13,6 +13,7 @@
 //
 // Sums of bfloat16 products stay in the tensor pipe over the whole contraction, which truncates each addition to float32: 2^-23
 // a step of 16, far below the result's rounding unless thousands of steps cancel.
+//
 // Float32 operands come as three bfloat16 parts (x 2^24 = h + m + l, exact); of the nine cross products six are formed,
 // the others are below 2^-25 of the product.  The tensor pipe adds with truncation, so an accumulator lives for one block
 // of 64 steps only (the corrections first, h.h last) and is then added to a float32 sum in registers, round to nearest.
@@ -694,8 +695,9 @@ int launch_kind(const DenseProduct& q, const DenseEpilogue& e, cudaStream_t st) 
 // that falls with the width, but by less than the width does, since A is staged as before (us with 256 / 192 / 128 columns,
 // the kernel alone after cold caches, ncu: 32768 tokens, 2048 x 768 forward 75.6 / 75.6 / 103, dx of 768 x 2048, k-major, 75.8 / 72.7 /
 // 82.6; 8192 tokens, 768 x 2048 25.9 / 27.2 / 32.5; 1000 tokens 11.9 / 10.7 / 10.7; float32 4001, 512 x 2048 forward 47.6 / 52.7 /
-// 45.2, where the rule takes 256, dx 43.0 / 45.2 / 41.2), and one for its epilogue.  Cutting the contraction fills the pairs where the output has few tiles, a weight gradient's or that of a few
-// hundred tokens; the parts are written and read once more, by one more launch.
+// 45.2, where the rule takes 256, dx 43.0 / 45.2 / 41.2), and one for its epilogue.  Cutting the contraction fills the pairs
+// where the output has few tiles, a weight gradient's or that of a few hundred tokens; the parts are written and read once more, by
+// one more launch.
 DenseTiling dense_tiling(DenseKind kind, bool f32, long long rows, long long cols, long long k) {
   const long long pairs = kChipSms / 2, m = (rows + 255) / 256, blocks = (k + kBK - 1) / kBK;
   const double step_us[3] = {f32 ? 3.0 : 0.40, f32 ? 2.25 : kind == kDenseDx ? 0.32 : 0.35, f32 ? 1.5 : 0.25};

@@ -9,8 +9,8 @@
 // in a fixed order.  64-deep pieces of W and x come in by cp.async, up to kStages at a time.  bfloat16: warp-level MMAs
 // (16 columns of W x 8 rows of x x 16 steps: with so few rows a tcgen05 tile would be padding, and the loads bound it in
 // either case); float32: fused multiply-adds.
-// One token, 768 x 2048, GELU: 6.0 us serialised by ncu for 3.1 MB of weights (the tile kernel 11), 48 rows, 2048 x 768 9.9 (14): there
-// 32 sums (8 slices of 4 parts of the steps) meet in each output, added up by 24 threads a block.
+// One token, 768 x 2048, GELU: 6.0 us serialised by ncu for 3.1 MB of weights (the tile kernel 11), 48 rows, 2048 x 768 9.9 (14):
+// there 32 sums (8 slices of 4 parts of the steps) meet in each output, added up by 24 threads a block.
 #include "linear_common.cuh"
 
 namespace swmoe {
